@@ -312,6 +312,132 @@ int shadowkv_argtopk(const double *scores, int32_t units, int32_t n, int32_t k, 
                      int32_t *out_ids, void *workspace, size_t workspace_bytes, void *stream);
 size_t shadowkv_argtopk_workspace_bytes(int32_t units, int32_t n, int32_t k);
 
+/*
+ * ---- The prompt's way into the cache: rotary positions, a paged KV cache, attention of new tokens over it ----
+ *
+ * Arrays of heads, [n_seqs, n_tokens, n_heads, d], are handed over with their strides (in elements); the d elements of
+ * a head are contiguous.  Pointers, and strides of dimensions longer than one, are multiples of 16 bytes, and no stride
+ * is negative.  An array that is written may not overlap itself or, unless a call says so, any other argument.  Ragged runs of
+ * tokens are one sequence of n_tokens = T tokens, cut by seq_starts.
+ */
+typedef struct shadowkv_heads {
+  void *data;                                    /* dev */
+  int64_t seq_stride, token_stride, head_stride; /* elements */
+  int32_t n_seqs, n_tokens, n_heads;             /* n_seqs and n_tokens may be 0 */
+  int32_t dtype;                                 /* SHADOWKV_KV_BF16 | SHADOWKV_KV_FP8_E5M2 */
+} shadowkv_heads;
+
+#define SHADOWKV_ROPE_HALF 0        /* pairs (i, i + rot_dim/2), as shadowkv_decode_step rotates */
+#define SHADOWKV_ROPE_INTERLEAVED 1 /* pairs (2i, 2i + 1) */
+
+/* Scaling of the frequencies w_i = theta^(-2i/rot_dim) for contexts longer than a model was trained on (f = factor): */
+#define SHADOWKV_ROPE_PLAIN 0       /* w_i */
+#define SHADOWKV_ROPE_LINEAR 1      /* w_i / f: positions interpolated */
+#define SHADOWKV_ROPE_NTK 2         /* theta replaced by theta * f^(rot_dim / (rot_dim - 2)); needs rot_dim > 2 */
+#define SHADOWKV_ROPE_BANDS 3       /* by the turns t_i = original_len w_i / 2 pi: w_i where t_i >= high, w_i / f where
+                                       t_i <= low, mixed linearly in t_i between; needs low < high */
+#define SHADOWKV_ROPE_YARN 4        /* by the index i: w_i up to the pair that makes `high` turns in original_len, w_i / f from
+                                       the one that makes `low` (> 0), mixed linearly between (their indices rounded outwards and
+                                       kept in [0, rot_dim - 1]) */
+
+typedef struct shadowkv_rope {
+  int32_t head_dim;     /* d in {64, 96, 128} */
+  int32_t rot_dim;      /* leading elements of a head that are rotated, a multiple of 8; 0 => head_dim */
+  int32_t layout;       /* SHADOWKV_ROPE_HALF | SHADOWKV_ROPE_INTERLEAVED */
+  int32_t scaling;      /* SHADOWKV_ROPE_PLAIN ... SHADOWKV_ROPE_YARN */
+  double theta;         /* > 0 (> 1 for YARN) */
+  double factor;        /* f > 0; ignored for PLAIN */
+  double low, high;     /* BANDS, YARN */
+  int32_t original_len; /* BANDS, YARN: > 0 */
+  int32_t reserved;     /* 0 */
+  double magnitude;     /* cosine and sine are multiplied by it; 0 => 1, and 0.1 ln f + 1 for YARN with f > 1 */
+  const float *inv_freq; /* optional dev [rot_dim/2]: replaces the frequencies; scaling must be PLAIN */
+} shadowkv_rope;
+
+/* The rot_dim/2 frequencies in radians per position, to host memory (fp64).  Rounded to fp32 on the device they are the
+ * inv_freq of shadowkv_params.  Returns SHADOWKV_OK or SHADOWKV_EINVAL (also where rope->inv_freq is set). */
+int shadowkv_rope_frequencies(const shadowkv_rope *rope, double *out);
+
+/*
+ * Turns every head of x to its token's position:  for a pair (x_i, x_j) with frequency w,
+ *   out_i = m (x_i cos(pos w) - x_j sin(pos w)),   out_j = m (x_j cos(pos w) + x_i sin(pos w));
+ * elements from rot_dim on are copied.  transposed != 0: with -pos in place of pos, which is the gradient with respect to
+ * x of a gradient with respect to out, and undoes the rotation where m = 1.  Angles are formed in fp64 and reduced to one
+ * turn, the rest is fp32, rounded once.
+ *
+ *   x          [n_seqs, n_tokens, n_heads, d]   bf16 or E5M2
+ *   out        same sizes, bf16 or E5M2, any strides; may be x itself (same pointer, type and strides)
+ *   positions  dev [n_seqs, n_tokens] int32 or NULL: position of every token
+ *   pos_offset dev [n_seqs] int32 or NULL (only with positions == NULL): token t of sequence i is at pos_offset[i] + t
+ * pre-RoPE keys [b, s, h_kv*d] turned into [b, h_kv, s, d] is one call with those strides.
+ */
+int shadowkv_rotate(const shadowkv_rope *rope, const shadowkv_heads *x, const shadowkv_heads *out,
+                    const int32_t *positions, const int32_t *pos_offset, int32_t transposed, void *stream);
+
+/*
+ * A cache of keys and values in pages of page_size tokens.  Row (page, head, row) of the keys is at
+ * k + page * k_page_stride + head * k_head_stride + row * k_token_stride elements, and likewise the values.  Token l of
+ * sequence i lies in page page_table[i * table_stride + l / page_size], row l % page_size.  An entry outside [0, n_pages)
+ * holds no tokens: what is appended there is dropped, and attention leaves its tokens out.
+ * A dense array [b, h_kv, cap, d] is such a cache with page_stride = page_size * d, head_stride = cap * d, pages
+ * (i * h_kv * cap) / page_size + j and n_pages = ((b - 1) * h_kv + 1) * cap / page_size.
+ */
+typedef struct shadowkv_paged_cache {
+  void *k, *v;                                          /* dev kv */
+  int64_t k_page_stride, k_head_stride, k_token_stride; /* elements */
+  int64_t v_page_stride, v_head_stride, v_token_stride;
+  const int32_t *page_table;                            /* dev [batch, table_stride], the first pages_per_seq used */
+  int64_t table_stride;
+  int32_t batch, pages_per_seq, n_pages;
+  int32_t n_kv_heads, head_dim;                         /* d in {64, 96, 128} */
+  int32_t page_size;                                    /* a power of two, up to 65536 */
+  int32_t kv_dtype;                                     /* SHADOWKV_KV_* */
+  int32_t reserved;                                     /* 0 */
+} shadowkv_paged_cache;
+
+/*
+ * Appends the keys and values of new tokens, rotating the keys (and the tokens' queries) on the way.  The new tokens of
+ * sequence i are rows seq_starts[i] .. seq_starts[i+1] - 1 of k, v and q; the j-th of its n_i goes to place
+ * l = kv_lens[i] - n_i + j of the sequence, and is rotated to position pos_offset[i] + l.  kv_lens therefore counts the new tokens,
+ * as shadowkv_paged_attention wants it.  Places below 0 or beyond pages_per_seq pages are dropped, as those on entries without a
+ * page; queries are turned all the same.  Rows outside every run are left as they were.
+ *
+ *   rope       NULL: keys are stored as they come; q and q_out must be NULL then
+ *   k, v       [1, T, h_kv, d]  bf16, or the cache's type; both the same
+ *   q, q_out   [1, T, h_q, d]   bf16 both, or both NULL; q_out may be q itself
+ *   seq_starts dev [batch + 1] int32, ascending; NULL: T / batch tokens of every sequence (batch must divide T)
+ *   kv_lens    dev [batch] int32
+ *   pos_offset dev [batch] int32 or NULL (0)
+ * No place may be written twice in a call.
+ */
+int shadowkv_paged_append(const shadowkv_paged_cache *cache, const shadowkv_rope *rope, const shadowkv_heads *k,
+                          const shadowkv_heads *v, const shadowkv_heads *q, const shadowkv_heads *q_out,
+                          const int32_t *seq_starts, const int32_t *kv_lens, const int32_t *pos_offset, void *stream);
+
+/*
+ * Attention of new tokens over the paged cache, which holds them already: for token j of the n_i of sequence i and query head g,
+ *   out = sum over the places l it sees of softmax_l(scale <q, k_l>) v_l   (KV head g / (h_q / h_kv)),
+ * where it sees l <= kv_lens[i] - n_i + j with causal != 0, else every l < kv_lens[i].  kv_lens is held to
+ * [0, pages_per_seq * page_size].  What a token does not see (later tokens, entries without a page, rows behind the
+ * length) has no influence on it, whatever is stored there, NaN and infinities among it.  A token that sees nothing, or whose logits
+ * are all minus infinity, gets out = 0 and lse = -inf.
+ *
+ *   q, out     [1, T, h_q, d] bf16; h_q / h_kv <= 64; rows outside every run are left as they were
+ *   lse        dev out [T, h_q] fp32 or NULL: natural logarithm of the sum of exp(scale <q, k_l>)
+ *   seq_starts, kv_lens  as shadowkv_paged_append
+ *   softmax_scale  0 => 1/sqrt(d)
+ *   workspace  dev >= shadowkv_paged_attention_workspace_bytes(), 256-byte aligned; its contents do not matter.  Two
+ *              calls whose work may overlap need a workspace each.
+ * Products and sums are fp32; the softmax weights are rounded to bf16 for the product with the values where a call has more than
+ * 32 rows (tokens x h_q / h_kv) a sequence on average, and enter as two bf16 terms otherwise.  Results do not depend on what else runs:
+ * the same call gives the same bits.
+ */
+int shadowkv_paged_attention(const shadowkv_paged_cache *cache, const shadowkv_heads *q, const shadowkv_heads *out,
+                             float *lse, const int32_t *seq_starts, const int32_t *kv_lens, int32_t causal,
+                             double softmax_scale, void *workspace, size_t workspace_bytes, void *stream);
+/* For n_tokens = T rows and h_q = n_q_heads (0 if the arguments are invalid; pointers are not looked at). */
+size_t shadowkv_paged_attention_workspace_bytes(const shadowkv_paged_cache *cache, int32_t n_q_heads, int32_t n_tokens);
+
 /* Workspace sizes in bytes for the given shape (0 if params are invalid). */
 size_t shadowkv_build_workspace_bytes(const shadowkv_params *params);
 size_t shadowkv_decode_workspace_bytes(const shadowkv_params *params);

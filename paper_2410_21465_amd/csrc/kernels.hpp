@@ -202,4 +202,61 @@ hipError_t launch_factorize(const void* k_pre, int kv_bytes, void* A, void* B, d
                             char* ws, const FactorizePlan& pl, int batch, int hkv, int d, int s, int s_cap, int r,
                             int n_iter, int n_sweeps, hipStream_t st);
 
+// ---- rotary positions and the paged cache (kernels_rope.hip, paged_attn_kernels.hpp) ----
+// An array of heads [seqs, tokens, heads, d], strides in bytes.
+struct HeadsArg {
+  uint8_t* p;
+  int64_t seq, tok, head;
+  int eb;                   // bytes per element: 2 = bf16, 1 = FP8 E5M2
+};
+struct RopeArgs {
+  int d, rot, interleaved;
+  float mag, sign;          // cosine and sine are multiplied by mag, the sine by sign too
+  const float* inv_freq;    // optional dev [rot/2]
+  double rev[kMaxHalfDim];  // revolutions per position
+};
+hipError_t launch_rotate(const RopeArgs& rope, const HeadsArg& x, const HeadsArg& out, const int32_t* positions,
+                         const int32_t* pos_offset, int n_seqs, int n_tokens, int n_heads, hipStream_t st);
+
+// Ragged runs of new tokens: rows seq_starts[i] .. seq_starts[i+1] - 1 of T belong to sequence i (NULL: T / batch each).
+struct RunsArg {
+  const int32_t* seq_starts;
+  const int32_t* kv_lens;
+  int batch, n_tokens;
+};
+struct PagesArg {           // one side (K or V) of a paged cache, strides in bytes
+  uint8_t* p;
+  int64_t page, head, tok;
+};
+struct PageTableArg {
+  const int32_t* table;     // [batch, stride]
+  int64_t stride;
+  int per_seq, n_pages, shift;   // shift: log2 of the page size
+};
+hipError_t launch_paged_append(const RopeArgs* rope, const PagesArg& kp, const PagesArg& vp, const PageTableArg& pt, int kv_bytes,
+                               const HeadsArg& k, const HeadsArg& v, const HeadsArg& q, const HeadsArg& q_out, int d, int hkv,
+                               int hq, const RunsArg& runs, const int32_t* pos_offset, hipStream_t st);
+
+struct PagedAttnArgs {
+  HeadsArg q, out;          // seq unused
+  float* lse;               // optional [T, hq]
+  PagesArg kp, vp;
+  PageTableArg pt;
+  RunsArg runs;
+  int hq, hkv, G, d, kv_bytes, causal;
+  float scale_log2;         // softmax scale * log2(e)
+  int tb;                   // tokens per row block
+  int n_wg;                 // workgroups the work is shared out to at most
+  int min_share;            // least work of a workgroup, in keys
+  int wide;                 // row offsets in 16-byte units pass 32 bits
+  int4* desc;               // [n_wg] {flags, sequence, KV head, row block} of the items that a workgroup leaves unfinished
+  float* part_acc;          // [2 n_wg, block rows, d] unnormalised sums
+  float2* part_ml;          // [2 n_wg, block rows] (max in log2 units, sum)
+};
+// Rows (tokens x query heads per KV head) of a row block: 16 or 32 where a workgroup's waves share out the keys, 128 where
+// they share out the rows.  rows: what a sequence has on average.
+int paged_attn_block_rows(int G, long rows);
+int paged_attn_workgroups(int block_rows);
+hipError_t launch_paged_attention(PagedAttnArgs a, int block_rows, hipStream_t st);
+
 }  // namespace skv

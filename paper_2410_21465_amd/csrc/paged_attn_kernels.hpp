@@ -1,0 +1,793 @@
+// Attention of new tokens over a paged cache (shadowkv_paged_attention):
+//   out = sum over the places l a row sees of softmax_l(scale <q, k_l>) v_l.
+// A row is one (token, query head); the G = h_q / h_kv rows of a token that share a KV head lie side by side in a block of rows, so
+// that K and V are read once for all of them.  One pass over the keys with a running maximum m and sum l in fp32 (log2 units):
+// a tile's logits S, m' = max(m, S), P = 2^(S - m'), l' = l 2^(m - m') + sum P, O' = O 2^(m - m') + P V, out = O / l.
+//
+// Both kernels form S^T = K Q^T, so that a lane of the matrix instruction's result holds one row's logits: the maximum
+// and the sum stay in the lane but for one exchange, the factors of a row are scalars of its lane, and P^T is already laid out as
+// the right operand of O^T = V^T P^T.  V^T is read from LDS with the transposing loads (ds_read_b64_tr_b16: lane i of 16 gets
+// column i of four rows of 16; checked on the chip).  The order of the keys inside a product is the one in which S^T leaves them.
+//
+// The work is shared out to at most n_wg workgroups without the host knowing any length.  An item is (sequence, KV head, row block), in
+// that order; its work is counted in keys, kItemKeys for itself and what its last row sees at most.  Workgroup w
+// takes the keys [w X / n, (w + 1) X / n) of the whole, X its sum, cut at tiles; an item that it leaves unfinished goes to the
+// workspace as (m, l, O), and a second kernel joins the parts in ascending order.  A long cache with few rows is split so, and many
+// short sequences are packed.
+#pragma once
+#include "kernels.hpp"
+
+namespace skv {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kItemKeys = 128;   // what starting and ending an item costs, in keys
+constexpr int kPartTail = 1, kPartHead = 2, kPartLast = 4;   // flags of a workgroup's unfinished items
+
+// ---- sharing out ----------------------------------------------------------------------------------------------------
+struct SeqRun {
+  int start, n, len;   // first row, new tokens, tokens in the cache
+};
+__device__ __forceinline__ SeqRun get_run(const RunsArg& r, const PageTableArg& pt, int i) {
+  SeqRun s;
+  if (r.seq_starts) {   // (held to [0, T]: whatever the array says, rows stay inside q and out)
+    const int lo = min(max(r.seq_starts[i], 0), r.n_tokens), hi = min(max(r.seq_starts[i + 1], 0), r.n_tokens);
+    s.start = lo;
+    s.n = max(0, hi - lo);
+  } else {
+    s.n = r.n_tokens / r.batch;
+    s.start = i * s.n;
+  }
+  s.len = (int)min((int64_t)max(r.kv_lens[i], 0), (int64_t)pt.per_seq << pt.shift);
+  return s;
+}
+// Work of one head of a sequence: block m's is base + slope (m + 1).
+struct SeqCost {
+  int64_t base, slope;
+  int blocks;
+  __device__ __forceinline__ int64_t before(int64_t m) const { return m * base + slope * (m * (m + 1) / 2); }
+  __device__ __forceinline__ int64_t head() const { return before(blocks); }
+};
+__device__ __forceinline__ SeqCost get_cost(const SeqRun& s, int tb, int causal) {
+  SeqCost c;
+  c.blocks = (s.n + tb - 1) / tb;
+  c.base = kItemKeys + (causal ? max(s.len - s.n, 0) : s.len);
+  c.slope = causal ? tb : 0;
+  return c;
+}
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {   // a value that all lanes hold, in scalar registers
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+struct Share {
+  int64_t x0, x1;      // this workgroup's part of the work
+  int w;               // its number
+  bool idle;           // there is no part for it
+  int seq, head, blk;  // the item in which x0 lies,
+  int64_t xs;          // and where that begins
+};
+
+// NT threads; lds: 2 * NT / 64 + 4 int64 of scratch.
+template <int NT>
+__device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* lds) {
+  constexpr int NW = NT / kWave;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, b = a.runs.batch;
+  int64_t total = 0;
+  for (int i = tid; i < b; i += NT) {
+    const SeqRun s = get_run(a.runs, a.pt, i);
+    total += get_cost(s, a.tb, a.causal).head() * a.hkv;
+  }
+  auto wave_sum = [](int64_t v) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) v += (int64_t)shfl_xor_u64((uint64_t)v, m);
+    return v;
+  };
+  total = wave_sum(total);
+  if (lane == 0) lds[wave] = total;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) total += lds[i];
+  total = uniform64(total);
+  Share sh;
+  const int64_t n64 = (total + a.min_share - 1) / a.min_share;
+  const int n = (int)(n64 < a.n_wg ? n64 : a.n_wg);
+  // neighbouring shares to one XCD (workgroups go round the eight of them), whose L2 then holds a head's K and V for all
+  // (n_wg is a multiple of eight, and every number below it is some workgroup's)
+  const int per = (n + 7) / 8, x = (int)blockIdx.x % 8, y = (int)blockIdx.x / 8, w = y < per ? x * per + y : 8 * y + x;
+  sh.w = w;
+  sh.idle = w >= n;
+  if (sh.idle) return sh;
+  const int64_t each = total / n, more = total % n;
+  sh.x0 = each * w + more * w / n;
+  sh.x1 = each * (w + 1) + more * (w + 1) / n;
+  int64_t before = 0;   // work of the sequences before the current NT
+  int64_t* found = lds + NW;
+  for (int i0 = 0; i0 < b; i0 += NT) {
+    const int i = i0 + tid;
+    SeqCost c{};
+    int64_t mine = 0;
+    if (i < b) {
+      c = get_cost(get_run(a.runs, a.pt, i), a.tb, a.causal);
+      mine = c.head() * a.hkv;
+    }
+    int64_t incl = mine;
+#pragma unroll
+    for (int m = 1; m < kWave; m <<= 1) {
+      const int64_t up = (int64_t)(((uint64_t)(uint32_t)__shfl_up((int)(incl >> 32), m, kWave) << 32) |
+                                   (uint32_t)__shfl_up((int)incl, m, kWave));
+      if (lane >= m) incl += up;
+    }
+    __syncthreads();
+    if (lane == kWave - 1) lds[wave] = incl;
+    __syncthreads();
+    int64_t base = before, all = 0;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      if (k < wave) base += lds[k];
+      all += lds[k];
+    }
+    const int64_t from = base + incl - mine;
+    if (mine > 0 && sh.x0 >= from && sh.x0 < from + mine) {
+      const int64_t head = c.head(), h = (sh.x0 - from) / head, rest = (sh.x0 - from) - h * head;
+      // the block: the largest m with before(m) <= rest
+      int64_t m;
+      if (c.slope == 0) {
+        m = rest / c.base;
+      } else {
+        const double p = (double)c.base / (double)c.slope + 0.5;
+        m = (int64_t)(sqrt(p * p + 2.0 * (double)rest / (double)c.slope) - p);
+        m = m < 0 ? 0 : m;
+        while (m > 0 && c.before(m) > rest) --m;
+        while (c.before(m + 1) <= rest) ++m;
+      }
+      found[0] = i;
+      found[1] = h;
+      found[2] = m;
+      found[3] = from + h * head + c.before(m);
+    }
+    before += all;
+  }
+  __syncthreads();
+  sh.seq = __builtin_amdgcn_readfirstlane((int)found[0]);
+  sh.head = __builtin_amdgcn_readfirstlane((int)found[1]);
+  sh.blk = __builtin_amdgcn_readfirstlane((int)found[2]);
+  sh.xs = uniform64(found[3]);
+  __syncthreads();
+  return sh;
+}
+
+// The workgroup's items one after the other: work(run, seq, head, blk, first tile, last tile + 1, tiles of the item, part slot or -1).
+template <int NT, int TILE, class F>
+__device__ __forceinline__ void for_items(const PagedAttnArgs& a, int64_t* lds, F&& work) {
+  const Share sh = get_share<NT>(a, lds);
+  if (sh.idle) {   // every entry of desc is written by every call
+    if (threadIdx.x == 0) a.desc[sh.w] = make_int4(0, 0, 0, 0);
+    return;
+  }
+  int4 desc = make_int4(0, 0, 0, 0);
+  int seq = sh.seq, head = sh.head, blk = sh.blk;
+  int64_t xs = sh.xs;
+  while (true) {
+    const SeqRun run = get_run(a.runs, a.pt, seq);
+    const SeqCost c = get_cost(run, a.tb, a.causal);
+    while (true) {
+      const int64_t cost = c.base + c.slope * (blk + 1);
+      const int seen = a.causal ? min(max(run.len - run.n + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
+      const int tiles = (seen + TILE - 1) / TILE;
+      auto tile_at = [&](int64_t p) {
+        return p >= cost ? tiles : p <= kItemKeys ? 0 : (int)min((int64_t)tiles, (p - kItemKeys) / TILE);
+      };
+      const int t0 = tile_at(sh.x0 - xs), t1 = tile_at(sh.x1 - xs);
+      if (t0 < t1 || (tiles == 0 && xs >= sh.x0)) {
+        int slot = -1;
+        if (t0 > 0) {
+          slot = 2 * sh.w;
+          desc.x |= kPartHead | (t1 == tiles ? kPartLast : 0);
+        } else if (t1 < tiles) {
+          slot = 2 * sh.w + 1;
+          desc = make_int4(desc.x | kPartTail, seq, head, blk);
+        }
+        work(run, seq, head, blk, t0, t1, slot);
+      }
+      xs += cost;
+      if (xs >= sh.x1) {
+        if (threadIdx.x == 0) a.desc[sh.w] = desc;
+        return;
+      }
+      if (++blk == c.blocks) {
+        blk = 0;
+        if (++head == a.hkv) break;
+      }
+    }
+    head = 0;
+    do ++seq; while (get_run(a.runs, a.pt, seq).n == 0);   // (xs < x1: there is one)
+  }
+}
+
+// ---- elements -------------------------------------------------------------------------------------------------------
+// two fp32 as two bf16, nearest even
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  const f2 x = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+// upper halves of two 32-bit words
+__device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+// four E5M2 bytes as four bf16 (exact)
+__device__ __forceinline__ uint2 e5m2x4_to_bf16(uint32_t w) {
+  const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_bf8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_bf8((int)w, true);
+  return make_uint2(upper_halves(__float_as_uint(lo[0]), __float_as_uint(lo[1])),
+                    upper_halves(__float_as_uint(hi[0]), __float_as_uint(hi[1])));
+}
+// whether one of two bf16 is infinite or NaN
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+// the same two with infinities and NaN as zero
+__device__ __forceinline__ uint32_t only_finite(uint32_t w) {
+  return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+}
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+// transposing load: four rows of 16 columns from the 16 lanes' addresses; lane i gets column i
+__device__ __forceinline__ uint2 read_tr(const uint8_t* p) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
+}
+__device__ __forceinline__ float max_halves(float x) {   // over lanes l and l ^ 32
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float max_quarters(float x) {  // over the four lanes l % 16
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float sum_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// Where a key's rows lie: the page of token `key`, and the offsets of its K and V rows (head excluded) in 16-byte units.  Keys
+// without a row get the cache's first one (in bounds; what is read there is masked out) and ok = false.
+struct KeyRow {
+  uint32_t k, v, k_hi, v_hi;
+  bool ok;
+};
+__device__ __forceinline__ int page_entry(const PagedAttnArgs& a, const int32_t* table, int key, int len) {
+  return key < len ? table[key >> a.pt.shift] : -1;
+}
+__device__ __forceinline__ KeyRow key_row(const PagedAttnArgs& a, int page, int key) {
+  KeyRow r;
+  r.ok = (unsigned)page < (unsigned)a.pt.n_pages;
+  const int64_t pg = r.ok ? page : 0;
+  const int64_t row = r.ok ? (key & ((1 << a.pt.shift) - 1)) : 0;
+  const uint64_t k = (uint64_t)(pg * (a.kp.page >> 4) + row * (a.kp.tok >> 4)), v = (uint64_t)(pg * (a.vp.page >> 4) + row * (a.vp.tok >> 4));
+  r.k = (uint32_t)k; r.k_hi = (uint32_t)(k >> 32);
+  r.v = (uint32_t)v; r.v_hi = (uint32_t)(v >> 32);
+  return r;
+}
+__device__ __forceinline__ uint64_t row_offset(uint32_t lo, uint32_t hi, int src, int wide) {   // bytes, of lane src's key
+  const uint32_t l = (uint32_t)__shfl((int)lo, src, kWave), h = wide ? (uint32_t)__shfl((int)hi, src, kWave) : 0u;
+  return (((uint64_t)h << 32) | l) << 4;
+}
+
+// ---- 128 rows: the four waves of a workgroup take 32 rows each -----------------------------------------------------------
+// Tiles of 64 keys, K and V through registers into two LDS buffers: while one tile is multiplied the next is on its way, one barrier a
+// tile.  FP8 is widened to bf16 between registers and LDS.  Per tile a wave issues 2 x D / 8 v_mfma_f32_32x32x16_bf16.
+// Row pitches: K's 16-byte reads of 16 rows and V's transposing reads of four rows of 64 bytes fall on all 64 banks.
+constexpr int kTileKeys = 64, kTileRows = 128, kTileNT = 256;
+template <int D>
+struct TilePitch {
+  static constexpr int k = 2 * D + 16;
+  static constexpr int v = D == 128 ? 320 : 192;
+  static constexpr int bytes = kTileKeys * (k + v);
+};
+
+template <int D, int EB>
+__global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnArgs a) {
+  constexpr int kPieces = D * EB / 16;                                   // 16-byte pieces of a row
+  constexpr int kLoads = (kTileKeys * kPieces + kTileNT - 1) / kTileNT;  // per thread, for K and for V
+  constexpr bool kEven = kTileKeys * kPieces % kTileNT == 0;
+  constexpr int PK = TilePitch<D>::k, PV = TilePitch<D>::v, QS = D / 16, DB = D / 32;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * TilePitch<D>::bytes];
+  __shared__ int64_t scratch[2 * kTileNT / kWave + 4];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, col = lane & 31, half = lane >> 5;
+
+  for_items<kTileNT, kTileKeys>(a, scratch, [&](const SeqRun& run, int seq, int head, int blk, int t0, int t1, int slot) {
+    const int G = a.G, row = wave * 32 + col, tl = row / G, g = row - tl * G, tok = blk * a.tb + tl;
+    const bool row_ok = tl < a.tb && tok < run.n;
+    const int limit = row_ok ? (a.causal ? run.len - run.n + tok : run.len - 1) : -1;   // last key the row sees
+    // tiles before `clear` are seen whole by every row of the block
+    const int first = a.causal ? run.len - run.n + blk * a.tb : run.len - 1, clear = max(first + 1, 0) / kTileKeys;
+    const int64_t qrow = run.start + tok;
+    bf16x8 qf[QS];
+    {
+      const uint8_t* qp = a.q.p + (row_ok ? qrow * a.q.tok + (head * G + g) * a.q.head : 0) + half * 16;
+#pragma unroll
+      for (int s = 0; s < QS; ++s) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (row_ok) w = *reinterpret_cast<const uint4*>(qp + s * 32);
+        qf[s] = __builtin_bit_cast(bf16x8, w);
+      }
+    }
+    f32x16 o[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    const int32_t* table = a.pt.table + seq * a.pt.stride;
+    const uint8_t* kbase = a.kp.p + head * a.kp.head;
+    const uint8_t* vbase = a.vp.p + head * a.vp.head;
+    uint4 kr[kLoads], vr[kLoads];
+    uint64_t have;            // keys of the staged tile that have a row
+    uint64_t have_now = 0;    // of the tile in use
+    auto request = [&](int t, int page) {
+      const int key = t * kTileKeys + lane;
+      const KeyRow kv = key_row(a, page, key);
+      have = __ballot(kv.ok);
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int p = tid + j * kTileNT;
+        if (kEven || p < kTileKeys * kPieces) {
+          const int r = p / kPieces, c = p - r * kPieces;
+          kr[j] = *reinterpret_cast<const uint4*>(kbase + row_offset(kv.k, kv.k_hi, r, a.wide) + c * 16);
+          vr[j] = *reinterpret_cast<const uint4*>(vbase + row_offset(kv.v, kv.v_hi, r, a.wide) + c * 16);
+        }
+      }
+    };
+    // registers -> LDS; with `check` says whether a value of the tile is infinite or NaN
+    auto store = [&](uint8_t* buf, bool check) {
+      bool odd = false;
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int p = tid + j * kTileNT;
+        if (kEven || p < kTileKeys * kPieces) {
+          const int r = p / kPieces, c = p - r * kPieces;
+          uint4 v = vr[j];
+          if (have != ~0ull && !((have >> r) & 1)) v = make_uint4(0, 0, 0, 0);
+          uint8_t* kd = buf + r * PK;
+          uint8_t* vd = buf + kTileKeys * PK + r * PV;
+          if constexpr (EB == 2) {
+            *reinterpret_cast<uint4*>(kd + c * 16) = kr[j];
+            *reinterpret_cast<uint4*>(vd + c * 16) = v;
+            if (check) odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
+          } else {
+            const uint2 k0 = e5m2x4_to_bf16(kr[j].x), k1 = e5m2x4_to_bf16(kr[j].y), k2 = e5m2x4_to_bf16(kr[j].z), k3 = e5m2x4_to_bf16(kr[j].w);
+            const uint2 v0 = e5m2x4_to_bf16(v.x), v1 = e5m2x4_to_bf16(v.y), v2 = e5m2x4_to_bf16(v.z), v3 = e5m2x4_to_bf16(v.w);
+            *reinterpret_cast<uint4*>(kd + c * 32) = make_uint4(k0.x, k0.y, k1.x, k1.y);
+            *reinterpret_cast<uint4*>(kd + c * 32 + 16) = make_uint4(k2.x, k2.y, k3.x, k3.y);
+            *reinterpret_cast<uint4*>(vd + c * 32) = make_uint4(v0.x, v0.y, v1.x, v1.y);
+            *reinterpret_cast<uint4*>(vd + c * 32 + 16) = make_uint4(v2.x, v2.y, v3.x, v3.y);
+            if (check) odd |= not_finite(v0.x) || not_finite(v0.y) || not_finite(v1.x) || not_finite(v1.y) || not_finite(v2.x) ||
+                              not_finite(v2.y) || not_finite(v3.x) || not_finite(v3.y);
+          }
+        }
+      }
+      have_now = have;
+      return odd;
+    };
+    auto masked = [&](int t, uint64_t h) { return t >= clear || h != ~0ull; };
+
+    bool odd_now = false;   // the tile in use is masked and has values that are infinite or NaN
+    int page = page_entry(a, table, t0 * kTileKeys + lane, run.len);
+    if (t0 < t1) {
+      request(t0, page);
+      page = page_entry(a, table, (t0 + 1) * kTileKeys + lane, run.len);
+      __syncthreads();   // (the buffers may still be read for the item before)
+      const bool check = masked(t0, have);
+      const bool odd = store(lds, check);
+      if (check) odd_now = __syncthreads_or(odd); else __syncthreads();
+    }
+    for (int t = t0; t < t1; ++t) {
+      uint8_t* buf = lds + (t - t0 & 1) * TilePitch<D>::bytes;
+      const uint64_t h = have_now;
+      if (t + 1 < t1) {
+        request(t + 1, page);
+        page = page_entry(a, table, (t + 2) * kTileKeys + lane, run.len);
+      }
+      f32x16 s[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[kb][j] = 0.f;
+        const uint8_t* kp = buf + (kb * 32 + col) * PK + half * 16;
+#pragma unroll
+        for (int i = 0; i < QS; ++i)
+          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kp + i * 32)), qf[i],
+                                                          s[kb], 0, 0, 0);
+      }
+      const bool mask = masked(t, h);
+      if (mask) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int k = kb * 32 + 8 * (j >> 2) + 4 * half + (j & 3);
+            if (t * kTileKeys + k > limit || !((h >> k) & 1)) s[kb][j] = -INFINITY;
+          }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) top = fmaxf(top, s[kb][j]);
+      top = max_halves(top) * a.scale_log2;
+      // The maximum follows the logits only where they pass it by 2^8: weights up to that lose nothing in bf16 or in fp32 sums.
+      if (__any(top > m + 8.f)) {
+        const float next = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
+        m = next;
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[i][j] *= f;
+      }
+      const float mm = m == -INFINITY ? 0.f : m;
+      uint32_t pw[2][8];
+      float sum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(s[kb][j] * a.scale_log2 - mm), p1 = __builtin_amdgcn_exp2f(s[kb][j + 1] * a.scale_log2 - mm);
+          sum += p0 + p1;
+          pw[kb][j >> 1] = pack_bf16(p0, p1);
+        }
+      l += sum;
+      const uint8_t* vp = buf + kTileKeys * PK + (4 * half + ((lane & 15) >> 2)) * PV + (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pw[kb][4 * u], pw[kb][4 * u + 1], pw[kb][4 * u + 2], pw[kb][4 * u + 3]));
+#pragma unroll
+          for (int i = 0; i < DB; ++i) {
+            uint2 x = read_tr(vp + (kb * 32 + u * 16) * PV + i * 64), y = read_tr(vp + (kb * 32 + u * 16 + 8) * PV + i * 64);
+            if (odd_now) x = make_uint2(only_finite(x.x), only_finite(x.y)), y = make_uint2(only_finite(y.x), only_finite(y.y));
+            o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y)), pf, o[i], 0, 0, 0);
+          }
+        }
+      if (odd_now) {
+        // infinities and NaN again, for the rows that see their keys
+        for (int k = 0; k < kTileKeys; ++k) {
+          if (t * kTileKeys + k > limit || !((h >> k) & 1)) continue;
+          const uint8_t* vk = buf + kTileKeys * PK + k * PV + half * 8;
+#pragma unroll
+          for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+              const uint2 w = *reinterpret_cast<const uint2*>(vk + i * 64 + j * 4);
+              const float e[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+#pragma unroll
+              for (int n = 0; n < 4; ++n)
+                if ((__float_as_uint(e[n]) & 0x7f800000u) == 0x7f800000u) o[i][j + n] += e[n];
+            }
+        }
+      }
+      if (t + 1 < t1) {
+        uint8_t* next = lds + ((t - t0 & 1) ^ 1) * TilePitch<D>::bytes;
+        const bool check = masked(t + 1, have);
+        const bool odd = store(next, check);
+        if (check) odd_now = __syncthreads_or(odd); else { odd_now = false; __syncthreads(); }
+      }
+    }
+
+    l = sum_halves(l);
+    if (slot < 0) {
+      if (!row_ok) return;
+      const float f = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+      uint8_t* dst = a.out.p + qrow * a.out.tok + (head * G + g) * a.out.head + half * 8;
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4)
+          *reinterpret_cast<uint2*>(dst + i * 64 + j * 4) = make_uint2(pack_bf16(o[i][j] * f, o[i][j + 1] * f), pack_bf16(o[i][j + 2] * f, o[i][j + 3] * f));
+      if (a.lse && half == 0) a.lse[qrow * a.hq + head * G + g] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    } else {
+      float* dst = a.part_acc + ((int64_t)slot * kTileRows + row) * D + half * 4;
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4)
+          *reinterpret_cast<float4*>(dst + i * 32 + j * 2) = make_float4(o[i][j], o[i][j + 1], o[i][j + 2], o[i][j + 3]);
+      if (half == 0) a.part_ml[(int64_t)slot * kTileRows + row] = make_float2(m, l);
+    }
+  });
+}
+
+// ---- 16 or 32 rows: the four waves of a workgroup take the keys in turn, 32 at a time ------------------------------------------
+// Bound by reading K and V.  K goes from memory straight into operand registers: of v_mfma_f32_16x16x32_bf16's left operand a lane
+// holds eight elements of one key, which four lanes of a row request as 64 neighbouring bytes; the order of the elements inside
+// the product is free as long as Q's is the same.  V goes through a piece of LDS of the wave's own, so nothing waits for
+// another wave before the end.  The next 32 keys are requested as soon as the registers are free.  The softmax weights enter as two bf16 terms:
+// the matrix pipe has the time (a wave's 32 keys take it 0.4 us x 1/2.4 of memory's).
+constexpr int kRowsKeys = 32, kRowsNT = 256;
+template <int D>
+struct RowsPitch {
+  static constexpr int v = 2 * D + 32;   // 32 bytes of eight rows on all 64 banks
+};
+
+template <int D, int EB, int NB>
+__global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnArgs a) {
+  constexpr int BR = 16 * NB, NW = kRowsNT / kWave, DB = D / 16;
+  constexpr int kSteps = D / 32;                          // products of 32 elements
+  constexpr int kPieces = D * EB / 16, kLoads = kRowsKeys * kPieces / kWave;   // V: 16-byte pieces of a row; per lane
+  constexpr int PV = RowsPitch<D>::v;
+  constexpr int kVBytes = NW * kRowsKeys * PV, kMergeBytes = NW * BR * (D * 4 + 8);
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kVBytes > kMergeBytes ? kVBytes : kMergeBytes];
+  __shared__ int64_t scratch[2 * kRowsNT / kWave + 4];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, col = lane & 15, quarter = lane >> 4;
+
+  for_items<kRowsNT, kRowsKeys * NW>(a, scratch, [&](const SeqRun& run, int seq, int head, int blk, int t0, int t1, int slot) {
+    const int G = a.G;
+    // Element order of step s: bf16, 32 s + 8 quarter + 0..7; FP8, whose 16-byte pieces hold 16 elements, steps 2 p and 2 p + 1
+    // take the halves of piece 64 p + 16 quarter (a last odd step 8-byte pieces).
+    auto elem = [&](int s) {
+      if (EB == 2 || (s == kSteps - 1 && kSteps % 2)) return 32 * s + 8 * quarter;
+      return 64 * (s / 2) + 16 * quarter + 8 * (s % 2);
+    };
+    bf16x8 qf[NB][kSteps];
+    int limit[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const int row = 16 * n + col, tl = row / G, g = row - tl * G, tok = blk * a.tb + tl;
+      const bool ok = tl < a.tb && tok < run.n;
+      limit[n] = ok ? (a.causal ? run.len - run.n + tok : run.len - 1) : -1;
+      const uint8_t* qp = a.q.p + (ok ? (run.start + tok) * a.q.tok + (head * G + g) * a.q.head : 0);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (ok) w = *reinterpret_cast<const uint4*>(qp + elem(s) * 2);
+        qf[n][s] = __builtin_bit_cast(bf16x8, w);
+      }
+    }
+    const int first = a.causal ? run.len - run.n + blk * a.tb : run.len - 1, clear = max(first + 1, 0) / kRowsKeys;
+    f32x4 o[NB][DB];
+    float m[NB], l[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      m[n] = -INFINITY;
+      l[n] = 0.f;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int32_t* table = a.pt.table + seq * a.pt.stride;
+    const uint8_t* kbase = a.kp.p + head * a.kp.head;
+    const uint8_t* vbase = a.vp.p + head * a.vp.head;
+    uint8_t* mine = lds + wave * kRowsKeys * PV;
+
+    constexpr int kW = (D * EB / 4 + 15) / 16;   // 16-byte pieces of K per lane and 16 keys (the last may be half used)
+    uint4 kr[2][kW], vr[kLoads];
+    KeyRow kv;             // of key (lane % 32) of the tile whose rows are requested next
+    uint32_t have = 0;
+    auto lookup = [&](int t) {
+      const int key = t * kRowsKeys + (lane & 31);
+      return page_entry(a, table, key, run.len);
+    };
+    auto request_k = [&]() {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const uint8_t* p = kbase + row_offset(kv.k, kv.k_hi, kb * 16 + col, a.wide);
+#pragma unroll
+        for (int s = 0; s < kW; ++s) {
+          if constexpr (EB == 1 && D % 64 != 0) {
+            if (s == kW - 1) {
+              const uint2 w = *reinterpret_cast<const uint2*>(p + s * 64 + 8 * quarter);
+              kr[kb][s] = make_uint4(w.x, w.y, 0, 0);
+              continue;
+            }
+          }
+          kr[kb][s] = *reinterpret_cast<const uint4*>(p + s * 64 + 16 * quarter);
+        }
+      }
+    };
+    auto request_v = [&]() {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int p = lane + j * kWave, r = p / kPieces, c = p - r * kPieces;
+        vr[j] = *reinterpret_cast<const uint4*>(vbase + row_offset(kv.v, kv.v_hi, r, a.wide) + c * 16);
+      }
+    };
+    const int seen = a.causal ? min(max(run.len - run.n + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
+    const int s0 = t0 * NW + wave, last = min(t1 * NW, (seen + kRowsKeys - 1) / kRowsKeys);   // in tiles of 32 keys
+    int page = -1;
+    if (s0 < last) {
+      kv = key_row(a, lookup(s0), s0 * kRowsKeys + (lane & 31));
+      have = (uint32_t)__ballot(kv.ok);
+      request_k();
+      request_v();
+      page = lookup(s0 + NW);
+    }
+    for (int t = s0; t < last; t += NW) {
+      const uint32_t h = have;
+      f32x4 s[NB][2];
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) s[n][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          bf16x8 kf;
+          if constexpr (EB == 2) {
+            kf = __builtin_bit_cast(bf16x8, kr[kb][i]);
+          } else {
+            const uint4 w = kr[kb][i / 2];
+            const uint2 x = e5m2x4_to_bf16(i % 2 ? w.z : w.x), y = e5m2x4_to_bf16(i % 2 ? w.w : w.y);
+            kf = __builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y));
+          }
+#pragma unroll
+          for (int n = 0; n < NB; ++n) s[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][i], s[n][kb], 0, 0, 0);
+        }
+      const bool more = t + NW < last;
+      if (more) {
+        kv = key_row(a, page, (t + NW) * kRowsKeys + (lane & 31));
+        have = (uint32_t)__ballot(kv.ok);
+        request_k();
+      }
+      const bool mask = t >= clear || h != ~0u;
+      bool odd = false;
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int p = lane + j * kWave, r = p / kPieces, c = p - r * kPieces;
+        uint4 v = vr[j];
+        if (h != ~0u && !((h >> r) & 1)) v = make_uint4(0, 0, 0, 0);
+        if constexpr (EB == 2) {
+          *reinterpret_cast<uint4*>(mine + r * PV + c * 16) = v;
+          if (mask) odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
+        } else {
+          const uint2 v0 = e5m2x4_to_bf16(v.x), v1 = e5m2x4_to_bf16(v.y), v2 = e5m2x4_to_bf16(v.z), v3 = e5m2x4_to_bf16(v.w);
+          *reinterpret_cast<uint4*>(mine + r * PV + c * 32) = make_uint4(v0.x, v0.y, v1.x, v1.y);
+          *reinterpret_cast<uint4*>(mine + r * PV + c * 32 + 16) = make_uint4(v2.x, v2.y, v3.x, v3.y);
+          if (mask) odd |= not_finite(v0.x) || not_finite(v0.y) || not_finite(v1.x) || not_finite(v1.y) || not_finite(v2.x) ||
+                           not_finite(v2.y) || not_finite(v3.x) || not_finite(v3.y);
+        }
+      }
+      odd = __any(odd);
+      if (more) {
+        request_v();
+        page = lookup(t + 2 * NW);
+      }
+      uint32_t ph[NB][4], pl[NB][4];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          x[j] = s[n][j >> 2][j & 3] * a.scale_log2;
+          const int k = 16 * (j >> 2) + 4 * quarter + (j & 3);
+          if (mask && (t * kRowsKeys + k > limit[n] || !((h >> k) & 1))) x[j] = -INFINITY;
+        }
+        float top = x[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
+        top = max_quarters(top);
+        if (__any(top > m[n] + 8.f)) {
+          const float next = fmaxf(m[n], top), f = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - next);
+          m[n] = next;
+          l[n] *= f;
+#pragma unroll
+          for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[n][i][j] *= f;
+        }
+        const float mm = m[n] == -INFINITY ? 0.f : m[n];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(x[j] - mm), p1 = __builtin_amdgcn_exp2f(x[j + 1] - mm);
+          l[n] += p0 + p1;
+          // the upper halves, and what they leave out (exact), rounded
+          const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+          ph[n][j >> 1] = upper_halves(u0, u1);
+          pl[n][j >> 1] = pack_bf16(p0 - __uint_as_float(u0 & 0xffff0000u), p1 - __uint_as_float(u1 & 0xffff0000u));
+        }
+      }
+      // V in the wave's LDS: written above by other lanes
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      const uint8_t* vp = mine + (4 * quarter + (col >> 2)) * PV + (col & 3) * 8;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) {
+        uint2 x = read_tr(vp + i * 32), y = read_tr(vp + 16 * PV + i * 32);
+        if (odd) x = make_uint2(only_finite(x.x), only_finite(x.y)), y = make_uint2(only_finite(y.x), only_finite(y.y));
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y));
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, make_uint4(ph[n][0], ph[n][1], ph[n][2], ph[n][3])),
+                                                            o[n][i], 0, 0, 0);
+          o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, make_uint4(pl[n][0], pl[n][1], pl[n][2], pl[n][3])),
+                                                            o[n][i], 0, 0, 0);
+        }
+      }
+      if (odd) {
+        for (int k = 0; k < kRowsKeys; ++k) {
+          if (!((h >> k) & 1)) continue;
+#pragma unroll
+          for (int i = 0; i < DB; ++i) {
+            const uint2 w = *reinterpret_cast<const uint2*>(mine + k * PV + i * 32 + quarter * 8);
+            const float e[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int n = 0; n < NB; ++n)
+                if (t * kRowsKeys + k <= limit[n] && (__float_as_uint(e[j]) & 0x7f800000u) == 0x7f800000u) o[n][i][j] += e[j];
+          }
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+
+    // the four waves' states
+    __syncthreads();   // (V's pieces of LDS are free)
+    float* macc = reinterpret_cast<float*>(lds);
+    float2* mml = reinterpret_cast<float2*>(lds + NW * BR * D * 4);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      l[n] = sum_quarters(l[n]);
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+        *reinterpret_cast<float4*>(macc + (wave * BR + 16 * n + col) * D + 16 * i + 4 * quarter) = make_float4(o[n][i][0], o[n][i][1], o[n][i][2], o[n][i][3]);
+      if (quarter == 0) mml[wave * BR + 16 * n + col] = make_float2(m[n], l[n]);
+    }
+    __syncthreads();
+    for (int p = tid; p < BR * D / 4; p += kRowsNT) {
+      const int row = p / (D / 4), c = (p - row * (D / 4)) * 4;
+      const int tl = row / G, g = row - tl * G, tok = blk * a.tb + tl;
+      if (tl >= a.tb || tok >= run.n) continue;
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) top = fmaxf(top, mml[w * BR + row].x);
+      float sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float2 ml = mml[w * BR + row];
+        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+        if (f == 0.f && ml.y == ml.y) continue;
+        const float4 v = *reinterpret_cast<const float4*>(macc + (w * BR + row) * D + c);
+        sum += ml.y * f;
+        x[0] += v.x * f; x[1] += v.y * f; x[2] += v.z * f; x[3] += v.w * f;
+      }
+      if (slot < 0) {
+        const float f = sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);
+        const int64_t qrow = run.start + tok;
+        *reinterpret_cast<uint2*>(a.out.p + qrow * a.out.tok + (head * G + g) * a.out.head + c * 2) =
+            make_uint2(pack_bf16(x[0] * f, x[1] * f), pack_bf16(x[2] * f, x[3] * f));
+        if (a.lse && c == 0) a.lse[qrow * a.hq + head * G + g] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+      } else {
+        *reinterpret_cast<float4*>(a.part_acc + ((int64_t)slot * BR + row) * D + c) = make_float4(x[0], x[1], x[2], x[3]);
+        if (c == 0) a.part_ml[(int64_t)slot * BR + row] = make_float2(top, sum);
+      }
+    }
+    __syncthreads();
+  });
+}
+
+template <int D, int EB>
+inline hipError_t launch_paged_attn_d(const PagedAttnArgs& a, int block_rows, hipStream_t st) {
+  if (block_rows == 16) hipLaunchKernelGGL((paged_attn_rows_kernel<D, EB, 1>), dim3(a.n_wg), dim3(kRowsNT), 0, st, a);
+  else if (block_rows == 32) hipLaunchKernelGGL((paged_attn_rows_kernel<D, EB, 2>), dim3(a.n_wg), dim3(kRowsNT), 0, st, a);
+  else hipLaunchKernelGGL((paged_attn_tiles_kernel<D, EB>), dim3(a.n_wg), dim3(kTileNT), 0, st, a);
+  return hipGetLastError();
+}
+template <int EB>
+inline hipError_t launch_paged_attn_eb(const PagedAttnArgs& a, int block_rows, hipStream_t st) {
+  return a.d == 64 ? launch_paged_attn_d<64, EB>(a, block_rows, st)
+         : a.d == 96 ? launch_paged_attn_d<96, EB>(a, block_rows, st) : launch_paged_attn_d<128, EB>(a, block_rows, st);
+}
+hipError_t launch_paged_attn_fp8(const PagedAttnArgs& a, int block_rows, hipStream_t st);   // kernels_paged_attn_fp8.hip
+
+}  // namespace skv

@@ -4,13 +4,12 @@
 #include "../../include/shadowkv.h"
 
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
 #include <vector>
 
+#include "api.hpp"
 #include "kernels.hpp"
 
 using namespace skv;
@@ -22,32 +21,6 @@ constexpr size_t kStaticScratchBytes = (size_t)96 << 20;
 static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 
 namespace {
-
-thread_local char g_err[512] = "";
-
-void set_err(const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof g_err, fmt, ap);
-  va_end(ap);
-}
-
-int fail_inval(const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof g_err, fmt, ap);
-  va_end(ap);
-  return SHADOWKV_EINVAL;
-}
-
-int fail_hip(const char* what, hipError_t e) {
-  set_err("%s: %s", what, hipGetErrorString(e));
-  return SHADOWKV_EHIP;
-}
-
-constexpr size_t kAlign = 256;
-size_t up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 struct Shape {
   int b, hq, hkv, G, d, s, c, r, o, k, w, n_ch, n_c, units;
@@ -231,13 +204,6 @@ bool build_layout(const Shape& sh, BuildLayout* L) {
   L->cand_idx = off; off += up((size_t)sh.units * L->sel.cand_stride * sizeof(int32_t));
   L->total = off;
   return true;
-}
-
-int check_workspace(void* ws, size_t have, size_t need) {
-  if (!ws) { set_err("workspace is NULL"); return SHADOWKV_EWORKSPACE; }
-  if (reinterpret_cast<uintptr_t>(ws) % kAlign) { set_err("workspace must be 256-byte aligned"); return SHADOWKV_EWORKSPACE; }
-  if (have < need) { set_err("workspace too small: %zu bytes given, %zu needed", have, need); return SHADOWKV_EWORKSPACE; }
-  return SHADOWKV_OK;
 }
 
 // Fork/join events, one pair per device, created on first use.

@@ -21,6 +21,8 @@ VALUES_DEVICE, VALUES_HOST = 0, 1
 FLAG_STAGE_VALUES = 1
 FLAG_KEEP_REBUILT_KEYS = 2
 KV_BF16, KV_FP8_E5M2 = 0, 1     # storage type of the KV-cache tensors (Params.kv_dtype)
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1                                        # Rope.layout
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3, 4  # Rope.scaling
 
 EXPORTS = (
     "shadowkv_build_landmarks", "shadowkv_decode_step", "shadowkv_build_workspace_bytes",
@@ -30,7 +32,8 @@ EXPORTS = (
     "shadowkv_value_cache_reset", "shadowkv_append_chunk", "shadowkv_argtopk", "shadowkv_argtopk_workspace_bytes",
     "shadowkv_factorize_keys", "shadowkv_factorize_workspace_bytes", "shadowkv_decode_step_static",
     "shadowkv_static_scratch_bytes", "shadowkv_decode_plan", "shadowkv_factorize_plan",
-    "shadowkv_decode_score_rows",
+    "shadowkv_decode_score_rows", "shadowkv_rope_frequencies", "shadowkv_rotate", "shadowkv_paged_append",
+    "shadowkv_paged_attention", "shadowkv_paged_attention_workspace_bytes",
 )
 STAGES = ("score", "select", "gather_values", "attention")
 
@@ -44,6 +47,26 @@ class CParams(C.Structure):
         ("rope_theta", C.c_double), ("softmax_scale", C.c_double), ("inv_freq", C.c_void_p),
         ("ctx_capacity", C.c_int32), ("kv_dtype", C.c_int32),
     ]
+
+
+class CHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("seq_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("n_heads", C.c_int32), ("dtype", C.c_int32)]
+
+
+class CRope(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("theta", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("original_len", C.c_int32), ("reserved", C.c_int32), ("magnitude", C.c_double), ("inv_freq", C.c_void_p)]
+
+
+class CPagedCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_page_stride", C.c_int64), ("k_head_stride", C.c_int64), ("k_token_stride", C.c_int64),
+                ("v_page_stride", C.c_int64), ("v_head_stride", C.c_int64), ("v_token_stride", C.c_int64),
+                ("page_table", C.c_void_p), ("table_stride", C.c_int64),
+                ("batch", C.c_int32), ("pages_per_seq", C.c_int32), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page_size", C.c_int32), ("kv_dtype", C.c_int32), ("reserved", C.c_int32)]
 
 
 class ShadowKVError(RuntimeError):
@@ -94,6 +117,16 @@ def lib() -> C.CDLL:
         L.shadowkv_factorize_plan.argtypes = [vp, vp]
         L.shadowkv_decode_score_rows.restype = i32
         L.shadowkv_decode_score_rows.argtypes = [vp]
+        L.shadowkv_rope_frequencies.restype = i32
+        L.shadowkv_rope_frequencies.argtypes = [vp, vp]
+        L.shadowkv_rotate.restype = i32
+        L.shadowkv_rotate.argtypes = [vp] * 5 + [i32, vp]
+        L.shadowkv_paged_append.restype = i32
+        L.shadowkv_paged_append.argtypes = [vp] * 10
+        L.shadowkv_paged_attention.restype = i32
+        L.shadowkv_paged_attention.argtypes = [vp] * 6 + [i32, C.c_double, vp, sz, vp]
+        L.shadowkv_paged_attention_workspace_bytes.restype = sz
+        L.shadowkv_paged_attention_workspace_bytes.argtypes = [vp, i32, i32]
         L.shadowkv_build_workspace_bytes.restype = sz
         L.shadowkv_build_workspace_bytes.argtypes = [vp]
         L.shadowkv_decode_workspace_bytes.restype = sz
@@ -462,3 +495,215 @@ def workspace_view(p: Params, workspace: torch.Tensor, which: str) -> Optional[t
     ld = (p.n_landmarks + 3) // 4 * 4
     n = p.batch * p.n_q_heads * ld
     return workspace[off:off + 4 * n].view(torch.float32).view(p.batch, p.n_q_heads, ld)[:, :, :p.n_landmarks]
+
+
+# ---- the prompt's way into the cache: rotary positions, a paged KV cache, attention of new tokens over it ----
+
+_DTYPES = {torch.bfloat16: KV_BF16, torch.float8_e5m2: KV_FP8_E5M2}
+
+
+@dataclass
+class Rope:
+    """Rotary positions (``shadowkv_rope``): which elements of a head turn, in which pairs, how fast."""
+    head_dim: int
+    theta: float = 5e5
+    rot_dim: int = 0                          # leading elements that are rotated, a multiple of 8 (0 => head_dim)
+    layout: int = ROPE_HALF                   # pairs (i, i + rot_dim/2), or ROPE_INTERLEAVED: (2i, 2i + 1)
+    scaling: int = ROPE_PLAIN                 # for long contexts: ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_YARN
+    factor: float = 1.0
+    low: float = 0.0                          # turns in original_len (BANDS, YARN)
+    high: float = 0.0
+    original_len: int = 0
+    magnitude: float = 0.0                    # of cosine and sine (0 => 1; YARN: 0.1 ln factor + 1)
+    inv_freq: Optional[torch.Tensor] = None   # device float32 [rot_dim/2], replaces the frequencies
+
+    def c_struct(self) -> CRope:
+        inv = None
+        if self.inv_freq is not None:
+            n = (self.rot_dim or self.head_dim) // 2
+            _want(self.inv_freq, "inv_freq", torch.float32, (n,))
+            inv = self.inv_freq.data_ptr()
+        return CRope(self.head_dim, self.rot_dim, self.layout, self.scaling, self.theta, self.factor, self.low, self.high,
+                     self.original_len, 0, self.magnitude, inv)
+
+    def frequencies(self) -> torch.Tensor:
+        """Radians per position of every pair, float64 on the host.  ``.float().cuda()`` is ``Params.inv_freq`` of a decode step
+        that rotates the same way (whole heads, half layout, magnitude 1)."""
+        out = torch.empty((self.rot_dim or self.head_dim) // 2, dtype=torch.float64)
+        st = self.c_struct()
+        _check(lib().shadowkv_rope_frequencies(C.byref(st), out.data_ptr()))
+        return out
+
+
+def _want(t: torch.Tensor, name: str, dtype, shape, device=None) -> None:
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be on {device or 'the GPU'}, not {t.device}")
+
+
+def _heads(t: torch.Tensor, name: str, device=None) -> CHeads:
+    """[seqs, tokens, heads, d] or [tokens, heads, d] with any strides as ``shadowkv_heads``."""
+    sz, st = t.shape, t.stride()
+    if len(sz) == 3:
+        seqs, seq_stride = 1, 0
+    elif len(sz) == 4:
+        seqs, seq_stride = sz[0], st[0]
+    else:
+        raise ValueError(f"{name} must have 3 or 4 dimensions, not {len(sz)}")
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{name} must be bfloat16 or float8_e5m2, not {t.dtype}")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be on {device or 'the GPU'}, not {t.device}")
+    if st[-1] != 1:
+        raise ValueError(f"the elements of a head of {name} must be contiguous")
+    return CHeads(t.data_ptr(), seq_stride, st[-3], st[-2], seqs, sz[-3], sz[-2], _DTYPES[t.dtype])
+
+
+class _Launch:
+    """Makes ``device`` current, and what is allocated inside belong to ``stream`` (None: the device's current stream)."""
+
+    def __init__(self, device: torch.device, stream):
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+        if stream is not None:
+            if stream.device != device:
+                raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+            self._ctx = torch.cuda.stream(stream)
+        else:
+            self._ctx = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+        self._device = device
+
+    def __enter__(self) -> int:
+        if self._ctx is not None:
+            self._ctx.__enter__()
+        return torch.cuda.current_stream(self._device).cuda_stream
+
+    def __exit__(self, *exc):
+        if self._ctx is not None:
+            self._ctx.__exit__(*exc)
+
+
+def rotate(rope: Rope, x: torch.Tensor, out: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+           pos_offset: Optional[torch.Tensor] = None, transposed: bool = False, stream=None) -> torch.Tensor:
+    """Heads ``x [seqs, tokens, heads, d]`` (or ``[tokens, heads, d]``) turned to their positions: ``positions [seqs, tokens]``
+    (``[tokens]``) int32, or ``pos_offset [seqs]`` + token.  ``out`` may have any strides (``k_rope.transpose(1, 2)`` of a
+    ``[seqs, heads, tokens, d]`` array), be of the other storage type, or be ``x``.  ``transposed`` turns back (the gradient)."""
+    dev = x.device
+    cx = _heads(x, "x")
+    if positions is not None:
+        _want(positions, "positions", torch.int32, x.shape[:-2], dev)
+    if pos_offset is not None:
+        _want(pos_offset, "pos_offset", torch.int32, (cx.n_seqs,), dev)
+    if x.shape[-1] != rope.head_dim or (out is not None and out.shape != x.shape):
+        raise ValueError(f"x must have heads of {rope.head_dim}, and out its shape")
+    if rope.inv_freq is not None and rope.inv_freq.device != dev:
+        raise ValueError("inv_freq must be on x's device")
+    with _Launch(dev, stream) as st:
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        cr, co = rope.c_struct(), _heads(out, "out", dev)
+        _check(lib().shadowkv_rotate(C.byref(cr), C.byref(cx), C.byref(co), None if positions is None else positions.data_ptr(),
+                                     None if pos_offset is None else pos_offset.data_ptr(), 1 if transposed else 0, st))
+    return out
+
+
+class PagedCache:
+    """Keys and values in pages: ``k, v [pages, h_kv, page_size, d]`` with any strides (the last 1), ``page_table [batch,
+    pages_per_seq]`` int32.  Entries outside ``[0, pages)`` hold no tokens.  Keeps the tensors; copies nothing."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor):
+        if k.dim() != 4 or v.shape != k.shape or k.dtype != v.dtype or k.dtype not in _DTYPES:
+            raise ValueError("k and v must be [pages, h_kv, page_size, d] arrays of one storage type")
+        if not k.is_cuda or v.device != k.device or page_table.device != k.device:
+            raise ValueError("k, v and page_table must be on one GPU")
+        ks, vs = k.stride(), v.stride()
+        if ks[3] != 1 or vs[3] != 1:
+            raise ValueError("the elements of a head must be contiguous")
+        if page_table.dim() != 2 or page_table.dtype != torch.int32 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table must be int32 [batch, pages_per_seq] with contiguous rows")
+        n, h, ps, d = k.shape
+        self.k, self.v, self.page_table, self.device = k, v, page_table, k.device
+        self.batch = page_table.shape[0]
+        self.c = CPagedCache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], page_table.data_ptr(),
+                             page_table.stride(0), self.batch, page_table.shape[1], n, h, d, ps, _DTYPES[k.dtype], 0)
+
+
+def dense_pages(k: torch.Tensor, v: torch.Tensor, page_size: int) -> PagedCache:
+    """A ``PagedCache`` on dense arrays ``k, v [b, h_kv, cap, d]`` (the value store, the keys of ``build_landmarks``): what is appended
+    there lies where those calls expect it.  ``page_size`` must divide ``cap``."""
+    if k.dim() != 4 or k.shape != v.shape or not k.is_contiguous() or not v.is_contiguous():
+        raise ValueError("k and v must be contiguous [b, h_kv, cap, d] arrays of one shape")
+    b, h, cap, d = k.shape
+    if b == 0 or page_size < 1 or cap % page_size:
+        raise ValueError(f"page_size {page_size} must divide the {cap} tokens of the arrays")
+    each = cap // page_size
+    shape, stride = ((b - 1) * h * each + each, h, page_size, d), (page_size * d, cap * d, d, 1)
+    table = (torch.arange(b, device=k.device)[:, None] * (h * each) + torch.arange(each, device=k.device)).to(torch.int32)
+    return PagedCache(k.as_strided(shape, stride), v.as_strided(shape, stride), table)
+
+
+def _runs(cache: PagedCache, kv_lens, seq_starts):
+    _want(kv_lens, "kv_lens", torch.int32, (cache.batch,), cache.device)
+    if seq_starts is not None:
+        _want(seq_starts, "seq_starts", torch.int32, (cache.batch + 1,), cache.device)
+    return None if seq_starts is None else seq_starts.data_ptr(), kv_lens.data_ptr()
+
+
+def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, kv_lens: torch.Tensor, seq_starts: Optional[torch.Tensor] = None,
+                 rope: Optional[Rope] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 pos_offset: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """Appends ``k, v [tokens, h_kv, d]`` to their sequences' pages, with ``rope`` the keys rotated on the way; ``q [tokens, h_q,
+    d]``, if given, is rotated beside them and returned (in ``q_out``, which may be ``q``).  Tokens ``seq_starts[i] ..
+    seq_starts[i+1]`` are sequence i's last ones of ``kv_lens[i]``; without ``seq_starts`` every sequence has as many."""
+    dev = cache.device
+    starts, lens = _runs(cache, kv_lens, seq_starts)
+    if k.dim() != 3 or v.dim() != 3 or k.shape[-1] != cache.c.head_dim or v.shape[-1] != cache.c.head_dim:
+        raise ValueError(f"k and v must be [tokens, h_kv, {cache.c.head_dim}]")
+    if q is not None and (q.dim() != 3 or q.shape[-1] != cache.c.head_dim or (q_out is not None and q_out.shape != q.shape)):
+        raise ValueError(f"q must be [tokens, h_q, {cache.c.head_dim}], and q_out of its shape")
+    if q is None and q_out is not None:
+        raise ValueError("q_out is given without q")
+    if pos_offset is not None:
+        _want(pos_offset, "pos_offset", torch.int32, (cache.batch,), dev)
+    if rope is not None and rope.inv_freq is not None and rope.inv_freq.device != dev:
+        raise ValueError("inv_freq must be on the cache's device")
+    with _Launch(dev, stream) as st:
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        ck, cv = _heads(k, "k", dev), _heads(v, "v", dev)
+        cq = C.byref(_heads(q, "q", dev)) if q is not None else None
+        co = C.byref(_heads(q_out, "q_out", dev)) if q is not None else None
+        cr = C.byref(rope.c_struct()) if rope is not None else None
+        _check(lib().shadowkv_paged_append(C.byref(cache.c), cr, C.byref(ck), C.byref(cv), cq, co, starts, lens,
+                                           None if pos_offset is None else pos_offset.data_ptr(), st))
+    return q_out
+
+
+def paged_attention_workspace_bytes(cache: PagedCache, n_q_heads: int, n_tokens: int) -> int:
+    return int(lib().shadowkv_paged_attention_workspace_bytes(C.byref(cache.c), n_q_heads, n_tokens))
+
+
+def paged_attention(cache: PagedCache, q: torch.Tensor, kv_lens: torch.Tensor, seq_starts: Optional[torch.Tensor] = None,
+                    causal: bool = True, softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of new tokens ``q [tokens, h_q, d]`` (after their rotation) over the pages, which hold their keys and values already.
+    Runs as in ``paged_append``.  Returns ``out`` (bf16, ``q``'s shape); ``lse [tokens, h_q]`` float32 is filled if given."""
+    dev = cache.device
+    starts, lens = _runs(cache, kv_lens, seq_starts)
+    if q.dim() != 3 or q.shape[-1] != cache.c.head_dim or (out is not None and out.shape != q.shape):
+        raise ValueError(f"q must be [tokens, h_q, {cache.c.head_dim}], and out of its shape")
+    if lse is not None:
+        _want(lse, "lse", torch.float32, q.shape[:2], dev)
+    with _Launch(dev, stream) as st:
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+        if workspace is None:
+            workspace = alloc_workspace(paged_attention_workspace_bytes(cache, q.shape[1], q.shape[0]), dev)
+        elif workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+        cq, co = _heads(q, "q", dev), _heads(out, "out", dev)
+        _check(lib().shadowkv_paged_attention(C.byref(cache.c), C.byref(cq), C.byref(co), None if lse is None else lse.data_ptr(), starts, lens,
+                                              1 if causal else 0, float(softmax_scale), workspace.data_ptr(),
+                                              workspace.numel() * workspace.element_size(), st))
+    return out
