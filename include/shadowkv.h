@@ -377,7 +377,8 @@ int shadowkv_rotate(const shadowkv_rope *rope, const shadowkv_heads *x, const sh
 /*
  * A cache of keys and values in pages of page_size tokens.  Row (page, head, row) of the keys is at
  * k + page * k_page_stride + head * k_head_stride + row * k_token_stride elements, and likewise the values.  Token l of
- * sequence i lies in page page_table[i * table_stride + l / page_size], row l % page_size.  An entry outside [0, n_pages)
+ * sequence i lies in page page_table[i * table_stride + l / page_size], row l % page_size.  The rows of one head span
+ * less than 64 GiB, and a sequence has room for 2^30 tokens at most.  An entry outside [0, n_pages)
  * holds no tokens: what is appended there is dropped, and attention leaves its tokens out.
  * A dense array [b, h_kv, cap, d] is such a cache with page_stride = page_size * d, head_stride = cap * d, pages
  * (i * h_kv * cap) / page_size + j and n_pages = ((b - 1) * h_kv + 1) * cap / page_size.

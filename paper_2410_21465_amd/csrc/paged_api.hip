@@ -148,6 +148,9 @@ int check_cache(const shadowkv_paged_cache* c, bool pointers, bool written) {
   const int64_t sz[3] = {c->n_pages, c->n_kv_heads, c->page_size};
   const int64_t ks[3] = {c->k_page_stride, c->k_head_stride, c->k_token_stride}, vs[3] = {c->v_page_stride, c->v_head_stride, c->v_token_stride};
   // (pages of a dense array lie inside each other's strides, so overlap is not looked for; a row has to have room)
+  for (const int64_t* st : {ks, vs})
+    if ((double)(c->n_pages - 1) * st[0] * eb + (double)(c->page_size - 1) * st[2] * eb >= 68719476736.0)
+      return fail_inval("the pages of a head span more than 64 GiB");
   int rc = check_strides("k pages", ks, sz, 3, c->head_dim, eb, false);
   if (rc == SHADOWKV_OK) rc = check_strides("v pages", vs, sz, 3, c->head_dim, eb, false);
   if (rc != SHADOWKV_OK || !written) return rc;
@@ -301,8 +304,6 @@ int shadowkv_paged_attention(const shadowkv_paged_cache* cache, const shadowkv_h
   a.tb = L.tb;
   a.n_wg = L.n_wg;
   a.min_share = 128;
-  auto units = [&](const PagesArg& p) { return (double)(cache->n_pages - 1) * p.page / 16 + (double)(cache->page_size - 1) * p.tok / 16; };
-  a.wide = std::max(units(a.kp), units(a.vp)) >= 4294967295.0;
   a.desc = reinterpret_cast<int4*>(ws + L.desc);
   a.part_acc = reinterpret_cast<float*>(ws + L.part_acc);
   a.part_ml = reinterpret_cast<float2*>(ws + L.part_ml);

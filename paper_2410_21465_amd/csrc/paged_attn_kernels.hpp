@@ -257,10 +257,10 @@ __device__ __forceinline__ float sum_quarters(float x) {
 }
 constexpr float kLn2 = 0.69314718055994530942f;
 
-// Where a key's rows lie: the page of token `key`, and the offsets of its K and V rows (head excluded) in 16-byte units.  Keys
+// Where a key's rows lie: offsets of its K and V rows (head excluded) in 16-byte units (the host sees to it that they fit).  Keys
 // without a row get the cache's first one (in bounds; what is read there is masked out) and ok = false.
 struct KeyRow {
-  uint32_t k, v, k_hi, v_hi;
+  uint32_t k, v;
   bool ok;
 };
 __device__ __forceinline__ int page_entry(const PagedAttnArgs& a, const int32_t* table, int key, int len) {
@@ -269,16 +269,13 @@ __device__ __forceinline__ int page_entry(const PagedAttnArgs& a, const int32_t*
 __device__ __forceinline__ KeyRow key_row(const PagedAttnArgs& a, int page, int key) {
   KeyRow r;
   r.ok = (unsigned)page < (unsigned)a.pt.n_pages;
-  const int64_t pg = r.ok ? page : 0;
-  const int64_t row = r.ok ? (key & ((1 << a.pt.shift) - 1)) : 0;
-  const uint64_t k = (uint64_t)(pg * (a.kp.page >> 4) + row * (a.kp.tok >> 4)), v = (uint64_t)(pg * (a.vp.page >> 4) + row * (a.vp.tok >> 4));
-  r.k = (uint32_t)k; r.k_hi = (uint32_t)(k >> 32);
-  r.v = (uint32_t)v; r.v_hi = (uint32_t)(v >> 32);
+  const uint32_t pg = r.ok ? page : 0, row = r.ok ? (key & ((1 << a.pt.shift) - 1)) : 0;
+  r.k = pg * (uint32_t)(a.kp.page >> 4) + row * (uint32_t)(a.kp.tok >> 4);
+  r.v = pg * (uint32_t)(a.vp.page >> 4) + row * (uint32_t)(a.vp.tok >> 4);
   return r;
 }
-__device__ __forceinline__ uint64_t row_offset(uint32_t lo, uint32_t hi, int src, int wide) {   // bytes, of lane src's key
-  const uint32_t l = (uint32_t)__shfl((int)lo, src, kWave), h = wide ? (uint32_t)__shfl((int)hi, src, kWave) : 0u;
-  return (((uint64_t)h << 32) | l) << 4;
+__device__ __forceinline__ uint64_t row_offset(uint32_t units, int src) {   // bytes, of lane src's key
+  return (uint64_t)(uint32_t)__shfl((int)units, src, kWave) << 4;
 }
 
 // ---- 128 rows: the four waves of a workgroup take 32 rows each -----------------------------------------------------------
@@ -302,6 +299,8 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * TilePitch<D>::bytes];
   __shared__ int64_t scratch[2 * kTileNT / kWave + 4];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, col = lane & 31, half = lane >> 5;
+  // this thread's pieces of a tile: piece pc of rows pr + j kRowStep (a row's pieces lie on neighbouring threads)
+  const int pr = tid / kPieces, pc = tid - pr * kPieces;
 
   for_items<kTileNT, kTileKeys>(a, scratch, [&](const SeqRun& run, int seq, int head, int blk, int t0, int t1, int slot) {
     const int G = a.G, row = wave * 32 + col, tl = row / G, g = row - tl * G, tok = blk * a.tb + tl;
@@ -330,94 +329,118 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
     const int32_t* table = a.pt.table + seq * a.pt.stride;
     const uint8_t* kbase = a.kp.p + head * a.kp.head;
     const uint8_t* vbase = a.vp.p + head * a.vp.head;
-    uint4 kr[kLoads], vr[kLoads];
-    uint64_t have;            // keys of the staged tile that have a row
-    uint64_t have_now = 0;    // of the tile in use
-    auto request = [&](int t, int page) {
-      const int key = t * kTileKeys + lane;
-      const KeyRow kv = key_row(a, page, key);
-      have = __ballot(kv.ok);
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const int p = tid + j * kTileNT;
-        if (kEven || p < kTileKeys * kPieces) {
-          const int r = p / kPieces, c = p - r * kPieces;
-          kr[j] = *reinterpret_cast<const uint4*>(kbase + row_offset(kv.k, kv.k_hi, r, a.wide) + c * 16);
-          vr[j] = *reinterpret_cast<const uint4*>(vbase + row_offset(kv.v, kv.v_hi, r, a.wide) + c * 16);
-        }
-      }
+    KeyRow kv{0, 0, false};   // of key `lane` of the tile on its way
+    uint64_t have = 0;        // keys of it that have a row
+    uint4 stage[kLoads];
+    // (a piece's row is found again from its number: j * 256 / kPieces rows on where that is whole)
+    auto piece = [&](int j, int& r, int& c) {
+      if constexpr (kTileNT % kPieces == 0) { r = pr + j * (kTileNT / kPieces); c = pc; }
+      else { const int p = tid + j * kTileNT; r = p / kPieces; c = p - r * kPieces; }
     };
-    // registers -> LDS; with `check` says whether a value of the tile is infinite or NaN
-    auto store = [&](uint8_t* buf, bool check) {
-      bool odd = false;
+    auto request = [&](const uint8_t* base, uint32_t units) {
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const int p = tid + j * kTileNT;
-        if (kEven || p < kTileKeys * kPieces) {
-          const int r = p / kPieces, c = p - r * kPieces;
-          uint4 v = vr[j];
-          if (have != ~0ull && !((have >> r) & 1)) v = make_uint4(0, 0, 0, 0);
-          uint8_t* kd = buf + r * PK;
-          uint8_t* vd = buf + kTileKeys * PK + r * PV;
+      for (int j = 0; j < kLoads; ++j)
+        if (kEven || tid + j * kTileNT < kTileKeys * kPieces) {
+          int r, c;
+          piece(j, r, c);
+          stage[j] = *reinterpret_cast<const uint4*>(base + row_offset(units, r) + c * 16);
+        }
+    };
+    // registers -> LDS, rows of a pitch
+    auto store = [&](uint8_t* dst, int pitch) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+        if (kEven || tid + j * kTileNT < kTileKeys * kPieces) {
+          int r, c;
+          piece(j, r, c);
+          uint8_t* d = dst + r * pitch + c * (32 / EB);
           if constexpr (EB == 2) {
-            *reinterpret_cast<uint4*>(kd + c * 16) = kr[j];
-            *reinterpret_cast<uint4*>(vd + c * 16) = v;
-            if (check) odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
+            *reinterpret_cast<uint4*>(d) = stage[j];
           } else {
-            const uint2 k0 = e5m2x4_to_bf16(kr[j].x), k1 = e5m2x4_to_bf16(kr[j].y), k2 = e5m2x4_to_bf16(kr[j].z), k3 = e5m2x4_to_bf16(kr[j].w);
-            const uint2 v0 = e5m2x4_to_bf16(v.x), v1 = e5m2x4_to_bf16(v.y), v2 = e5m2x4_to_bf16(v.z), v3 = e5m2x4_to_bf16(v.w);
-            *reinterpret_cast<uint4*>(kd + c * 32) = make_uint4(k0.x, k0.y, k1.x, k1.y);
-            *reinterpret_cast<uint4*>(kd + c * 32 + 16) = make_uint4(k2.x, k2.y, k3.x, k3.y);
-            *reinterpret_cast<uint4*>(vd + c * 32) = make_uint4(v0.x, v0.y, v1.x, v1.y);
-            *reinterpret_cast<uint4*>(vd + c * 32 + 16) = make_uint4(v2.x, v2.y, v3.x, v3.y);
-            if (check) odd |= not_finite(v0.x) || not_finite(v0.y) || not_finite(v1.x) || not_finite(v1.y) || not_finite(v2.x) ||
-                              not_finite(v2.y) || not_finite(v3.x) || not_finite(v3.y);
+            const uint2 w0 = e5m2x4_to_bf16(stage[j].x), w1 = e5m2x4_to_bf16(stage[j].y), w2 = e5m2x4_to_bf16(stage[j].z), w3 = e5m2x4_to_bf16(stage[j].w);
+            *reinterpret_cast<uint4*>(d) = make_uint4(w0.x, w0.y, w1.x, w1.y);
+            *reinterpret_cast<uint4*>(d + 16) = make_uint4(w2.x, w2.y, w3.x, w3.y);
           }
         }
-      }
-      have_now = have;
-      return odd;
     };
-    auto masked = [&](int t, uint64_t h) { return t >= clear || h != ~0ull; };
+    // Values of keys without a row become zero, since a weight of zero does not make NaN harmless; whether any is infinite or NaN.
+    auto clean = [&]() {
+      uint32_t odd = 0;
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+        if (kEven || tid + j * kTileNT < kTileKeys * kPieces) {
+          int r, c;
+          piece(j, r, c);
+          if (!((have >> r) & 1)) stage[j] = make_uint4(0, 0, 0, 0);
+          const uint32_t w[4] = {stage[j].x, stage[j].y, stage[j].z, stage[j].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            odd |= EB == 2 ? not_finite(w[e]) : (w[e] & 0x7cu) == 0x7cu || (w[e] & 0x7c00u) == 0x7c00u || (w[e] & 0x7c0000u) == 0x7c0000u || (w[e] & 0x7c000000u) == 0x7c000000u;
+        }
+      return odd != 0;
+    };
+    auto masked = [&](int t) { return t >= clear || have != ~0ull; };
 
-    bool odd_now = false;   // the tile in use is masked and has values that are infinite or NaN
+    bool mask = false, odd = false;   // of the tile in use: not all seen by all; of its values some are infinite or NaN
+    uint64_t have_now = 0;
     int page = page_entry(a, table, t0 * kTileKeys + lane, run.len);
     if (t0 < t1) {
-      request(t0, page);
+      kv = key_row(a, page, t0 * kTileKeys + lane);
+      have_now = have = __ballot(kv.ok);
       page = page_entry(a, table, (t0 + 1) * kTileKeys + lane, run.len);
+      request(kbase, kv.k);
       __syncthreads();   // (the buffers may still be read for the item before)
-      const bool check = masked(t0, have);
-      const bool odd = store(lds, check);
-      if (check) odd_now = __syncthreads_or(odd); else __syncthreads();
+      store(lds, PK);
+      request(vbase, kv.v);
+      mask = masked(t0);
+      bool bad = false;
+      if (mask) bad = clean();
+      store(lds + kTileKeys * PK, PV);
+      if (mask) odd = __syncthreads_or(bad); else __syncthreads();
     }
+#pragma unroll 1
     for (int t = t0; t < t1; ++t) {
-      uint8_t* buf = lds + (t - t0 & 1) * TilePitch<D>::bytes;
-      const uint64_t h = have_now;
-      if (t + 1 < t1) {
-        request(t + 1, page);
+      uint8_t* buf = lds + ((t - t0) & 1) * TilePitch<D>::bytes;
+      uint8_t* next = lds + (((t - t0) & 1) ^ 1) * TilePitch<D>::bytes;
+      const bool more = t + 1 < t1;
+      if (more) {
+        kv = key_row(a, page, (t + 1) * kTileKeys + lane);
+        have = __ballot(kv.ok);
         page = page_entry(a, table, (t + 2) * kTileKeys + lane, run.len);
+        request(kbase, kv.k);
       }
+      __builtin_amdgcn_sched_barrier(0);
       f32x16 s[2];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[kb][j] = 0.f;
-        const uint8_t* kp = buf + (kb * 32 + col) * PK + half * 16;
+      {
+        const uint8_t* kp = buf + col * PK + half * 16;
 #pragma unroll
         for (int i = 0; i < QS; ++i)
-          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kp + i * 32)), qf[i],
-                                                          s[kb], 0, 0, 0);
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kp + kb * 32 * PK + i * 32)), qf[i], s[kb], 0, 0, 0);
       }
-      const bool mask = masked(t, h);
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) {
+        store(next, PK);
+        request(vbase, kv.v);
+      }
       if (mask) {
+        const int rel = limit - t * kTileKeys - 4 * half;
+        const uint64_t h = have_now >> (4 * half);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            const int k = kb * 32 + 8 * (j >> 2) + 4 * half + (j & 3);
-            if (t * kTileKeys + k > limit || !((h >> k) & 1)) s[kb][j] = -INFINITY;
+            const int k = kb * 32 + 8 * (j >> 2) + (j & 3);
+            if (k > rel || !((h >> k) & 1)) s[kb][j] = -INFINITY;
           }
       }
+      __builtin_amdgcn_sched_barrier(0);
       float top = s[0][0];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -426,8 +449,8 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
       top = max_halves(top) * a.scale_log2;
       // The maximum follows the logits only where they pass it by 2^8: weights up to that lose nothing in bf16 or in fp32 sums.
       if (__any(top > m + 8.f)) {
-        const float next = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
-        m = next;
+        const float next_m = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next_m);
+        m = next_m;
         l *= f;
 #pragma unroll
         for (int i = 0; i < DB; ++i)
@@ -446,7 +469,31 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
           pw[kb][j >> 1] = pack_bf16(p0, p1);
         }
       l += sum;
-      const uint8_t* vp = buf + kTileKeys * PK + (4 * half + ((lane & 15) >> 2)) * PV + (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+      uint8_t* vt = buf + kTileKeys * PK;
+      if (odd) {
+        // infinities and NaN go to the rows that see their keys, and are zero for the product
+        for (int k = 0; k < kTileKeys; ++k) {
+          if (t * kTileKeys + k > limit || !((have_now >> k) & 1)) continue;
+#pragma unroll
+          for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+              const uint2 w = *reinterpret_cast<const uint2*>(vt + k * PV + half * 8 + i * 64 + j * 4);
+              const float e[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+#pragma unroll
+              for (int n = 0; n < 4; ++n)
+                if ((__float_as_uint(e[n]) & 0x7f800000u) == 0x7f800000u) o[i][j + n] += e[n];
+            }
+        }
+        __syncthreads();
+        for (int p = tid; p < kTileKeys * D / 4; p += kTileNT) {
+          uint2* w = reinterpret_cast<uint2*>(vt + p / (D / 4) * PV + p % (D / 4) * 8);
+          *w = make_uint2(only_finite(w->x), only_finite(w->y));
+        }
+        __syncthreads();
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const uint8_t* vp = vt + (4 * half + ((lane & 15) >> 2)) * PV + (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -454,33 +501,18 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
           const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pw[kb][4 * u], pw[kb][4 * u + 1], pw[kb][4 * u + 2], pw[kb][4 * u + 3]));
 #pragma unroll
           for (int i = 0; i < DB; ++i) {
-            uint2 x = read_tr(vp + (kb * 32 + u * 16) * PV + i * 64), y = read_tr(vp + (kb * 32 + u * 16 + 8) * PV + i * 64);
-            if (odd_now) x = make_uint2(only_finite(x.x), only_finite(x.y)), y = make_uint2(only_finite(y.x), only_finite(y.y));
+            const uint2 x = read_tr(vp + (kb * 32 + u * 16) * PV + i * 64), y = read_tr(vp + (kb * 32 + u * 16 + 8) * PV + i * 64);
             o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y)), pf, o[i], 0, 0, 0);
           }
         }
-      if (odd_now) {
-        // infinities and NaN again, for the rows that see their keys
-        for (int k = 0; k < kTileKeys; ++k) {
-          if (t * kTileKeys + k > limit || !((h >> k) & 1)) continue;
-          const uint8_t* vk = buf + kTileKeys * PK + k * PV + half * 8;
-#pragma unroll
-          for (int i = 0; i < DB; ++i)
-#pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-              const uint2 w = *reinterpret_cast<const uint2*>(vk + i * 64 + j * 4);
-              const float e[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
-#pragma unroll
-              for (int n = 0; n < 4; ++n)
-                if ((__float_as_uint(e[n]) & 0x7f800000u) == 0x7f800000u) o[i][j + n] += e[n];
-            }
-        }
-      }
-      if (t + 1 < t1) {
-        uint8_t* next = lds + ((t - t0 & 1) ^ 1) * TilePitch<D>::bytes;
-        const bool check = masked(t + 1, have);
-        const bool odd = store(next, check);
-        if (check) odd_now = __syncthreads_or(odd); else { odd_now = false; __syncthreads(); }
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) {
+        mask = masked(t + 1);
+        bool bad = false;
+        if (mask) bad = clean();
+        store(next + kTileKeys * PK, PV);
+        have_now = have;
+        if (mask) odd = __syncthreads_or(bad); else { odd = false; __syncthreads(); }
       }
     }
 
@@ -579,7 +611,7 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
     auto request_k = [&]() {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        const uint8_t* p = kbase + row_offset(kv.k, kv.k_hi, kb * 16 + col, a.wide);
+        const uint8_t* p = kbase + row_offset(kv.k, kb * 16 + col);
 #pragma unroll
         for (int s = 0; s < kW; ++s) {
           if constexpr (EB == 1 && D % 64 != 0) {
@@ -597,7 +629,7 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         const int p = lane + j * kWave, r = p / kPieces, c = p - r * kPieces;
-        vr[j] = *reinterpret_cast<const uint4*>(vbase + row_offset(kv.v, kv.v_hi, r, a.wide) + c * 16);
+        vr[j] = *reinterpret_cast<const uint4*>(vbase + row_offset(kv.v, r) + c * 16);
       }
     };
     const int seen = a.causal ? min(max(run.len - run.n + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
