@@ -263,12 +263,13 @@ struct KeyRow {
   uint32_t k, v;
   bool ok;
 };
+// (always a load, of the last token's entry for keys behind it: whether the key has a row is asked when the entry is used)
 __device__ __forceinline__ int page_entry(const PagedAttnArgs& a, const int32_t* table, int key, int len) {
-  return key < len ? table[key >> a.pt.shift] : -1;
+  return table[min(key, len - 1) >> a.pt.shift];
 }
-__device__ __forceinline__ KeyRow key_row(const PagedAttnArgs& a, int page, int key) {
+__device__ __forceinline__ KeyRow key_row(const PagedAttnArgs& a, int page, int key, int len) {
   KeyRow r;
-  r.ok = (unsigned)page < (unsigned)a.pt.n_pages;
+  r.ok = key < len && (unsigned)page < (unsigned)a.pt.n_pages;
   const uint32_t pg = r.ok ? page : 0, row = r.ok ? (key & ((1 << a.pt.shift) - 1)) : 0;
   r.k = pg * (uint32_t)(a.kp.page >> 4) + row * (uint32_t)(a.kp.tok >> 4);
   r.v = pg * (uint32_t)(a.vp.page >> 4) + row * (uint32_t)(a.vp.tok >> 4);
@@ -337,13 +338,23 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
       if constexpr (kTileNT % kPieces == 0) { r = pr + j * (kTileNT / kPieces); c = pc; }
       else { const int p = tid + j * kTileNT; r = p / kPieces; c = p - r * kPieces; }
     };
-    auto request = [&](const uint8_t* base, uint32_t units) {
+    uint32_t at_k[kLoads], at_v[kLoads];   // where the rows of this thread's pieces lie, from the lanes that looked them up
+    auto locate = [&]() {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        int r, c;
+        piece(j, r, c);
+        at_k[j] = (uint32_t)__shfl((int)kv.k, r, kWave);
+        at_v[j] = (uint32_t)__shfl((int)kv.v, r, kWave);
+      }
+    };
+    auto request = [&](const uint8_t* base, const uint32_t (&at)[kLoads]) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j)
         if (kEven || tid + j * kTileNT < kTileKeys * kPieces) {
           int r, c;
           piece(j, r, c);
-          stage[j] = *reinterpret_cast<const uint4*>(base + row_offset(units, r) + c * 16);
+          stage[j] = *reinterpret_cast<const uint4*>(base + ((uint64_t)at[j] << 4) + c * 16);
         }
     };
     // registers -> LDS, rows of a pitch
@@ -383,15 +394,17 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
 
     bool mask = false, odd = false;   // of the tile in use: not all seen by all; of its values some are infinite or NaN
     uint64_t have_now = 0;
-    int page = page_entry(a, table, t0 * kTileKeys + lane, run.len);
-    if (t0 < t1) {
-      kv = key_row(a, page, t0 * kTileKeys + lane);
+    int page_next = 0;
+    if (t0 < t1) {   // (so run.len > 0)
+      int page = page_entry(a, table, t0 * kTileKeys + lane, run.len);
+      kv = key_row(a, page, t0 * kTileKeys + lane, run.len);
+      page_next = page_entry(a, table, (t0 + 1) * kTileKeys + lane, run.len);
       have_now = have = __ballot(kv.ok);
-      page = page_entry(a, table, (t0 + 1) * kTileKeys + lane, run.len);
-      request(kbase, kv.k);
+      locate();
+      request(kbase, at_k);
       __syncthreads();   // (the buffers may still be read for the item before)
       store(lds, PK);
-      request(vbase, kv.v);
+      request(vbase, at_v);
       mask = masked(t0);
       bool bad = false;
       if (mask) bad = clean();
@@ -402,45 +415,55 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
     for (int t = t0; t < t1; ++t) {
       uint8_t* buf = lds + ((t - t0) & 1) * TilePitch<D>::bytes;
       uint8_t* next = lds + (((t - t0) & 1) ^ 1) * TilePitch<D>::bytes;
-      const bool more = t + 1 < t1;
-      if (more) {
-        kv = key_row(a, page, (t + 1) * kTileKeys + lane);
-        have = __ballot(kv.ok);
-        page = page_entry(a, table, (t + 2) * kTileKeys + lane, run.len);
-        request(kbase, kv.k);
-      }
-      __builtin_amdgcn_sched_barrier(0);
+      // The next tile, or behind the last one (t + 1 == t1) whatever follows, which nothing uses: no branch, so that the loads stay
+      // in flight (where a branch joined them, the compiler's copies waited for them at once: 715 TFLOP/s against %NEW%).
+      kv = key_row(a, page_next, (t + 1) * kTileKeys + lane, run.len);
+      page_next = page_entry(a, table, (t + 2) * kTileKeys + lane, run.len);
+      have = __ballot(kv.ok);
+      locate();
+      request(kbase, at_k);
       f32x16 s[2];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[kb][j] = 0.f;
       {
+        // operands of two products per key block are read while the two before are multiplied
         const uint8_t* kp = buf + col * PK + half * 16;
+        uint4 kf[2][4];
+        auto read = [&](int i, uint4 (&f)[4]) {
 #pragma unroll
-        for (int i = 0; i < QS; ++i)
+          for (int e = 0; e < 4; ++e) f[e] = *reinterpret_cast<const uint4*>(kp + (e & 1) * 32 * PK + (i + (e >> 1)) * 32);
+        };
+        read(0, kf[0]);
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kp + kb * 32 * PK + i * 32)), qf[i], s[kb], 0, 0, 0);
+        for (int i = 0; i < QS; i += 2) {
+          if (i + 2 < QS) read(i + 2, kf[(i / 2 + 1) % 2]);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            s[e & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[i / 2 % 2][e]), qf[i + (e >> 1)], s[e & 1], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-      __builtin_amdgcn_sched_barrier(0);
-      if (more) {
-        store(next, PK);
-        request(vbase, kv.v);
-      }
+      store(next, PK);
+      request(vbase, at_v);
       if (mask) {
         const int rel = limit - t * kTileKeys - 4 * half;
-        const uint64_t h = have_now >> (4 * half);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int k = kb * 32 + 8 * (j >> 2) + (j & 3);
-            if (k > rel || !((h >> k) & 1)) s[kb][j] = -INFINITY;
-          }
+          for (int j = 0; j < 16; ++j)
+            if (kb * 32 + 8 * (j >> 2) + (j & 3) > rel) s[kb][j] = -INFINITY;
+        if (have_now != ~0ull) {
+          const uint64_t h = have_now >> (4 * half);
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (!((h >> (kb * 32 + 8 * (j >> 2) + (j & 3))) & 1)) s[kb][j] = -INFINITY;
+        }
       }
-      __builtin_amdgcn_sched_barrier(0);
       float top = s[0][0];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -492,28 +515,34 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
         }
         __syncthreads();
       }
-      __builtin_amdgcn_sched_barrier(0);
-      const uint8_t* vp = vt + (4 * half + ((lane & 15) >> 2)) * PV + (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pw[kb][4 * u], pw[kb][4 * u + 1], pw[kb][4 * u + 2], pw[kb][4 * u + 3]));
+      {
+        const uint8_t* vp = vt + (4 * half + ((lane & 15) >> 2)) * PV + (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+        uint4 vf[2][DB];
+        auto read = [&](int u, uint4 (&f)[DB]) {   // 16 keys
 #pragma unroll
           for (int i = 0; i < DB; ++i) {
-            const uint2 x = read_tr(vp + (kb * 32 + u * 16) * PV + i * 64), y = read_tr(vp + (kb * 32 + u * 16 + 8) * PV + i * 64);
-            o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y)), pf, o[i], 0, 0, 0);
+            const uint2 x = read_tr(vp + u * 16 * PV + i * 64), y = read_tr(vp + (u * 16 + 8) * PV + i * 64);
+            f[i] = make_uint4(x.x, x.y, y.x, y.y);
           }
+        };
+        read(0, vf[0]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (u < 3) read(u + 1, vf[(u + 1) % 2]);
+          __builtin_amdgcn_sched_barrier(0);
+          const uint32_t* p = pw[u / 2] + 4 * (u % 2);
+          const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(p[0], p[1], p[2], p[3]));
+#pragma unroll
+          for (int i = 0; i < DB; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[u % 2][i]), pf, o[i], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
         }
-      __builtin_amdgcn_sched_barrier(0);
-      if (more) {
-        mask = masked(t + 1);
-        bool bad = false;
-        if (mask) bad = clean();
-        store(next + kTileKeys * PK, PV);
-        have_now = have;
-        if (mask) odd = __syncthreads_or(bad); else { odd = false; __syncthreads(); }
       }
+      mask = t + 1 < t1 && masked(t + 1);
+      bool bad = false;
+      if (mask) bad = clean();
+      store(next + kTileKeys * PK, PV);
+      have_now = have;
+      if (mask) odd = __syncthreads_or(bad); else { odd = false; __syncthreads(); }
     }
 
     l = sum_halves(l);
@@ -636,7 +665,7 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
     const int s0 = t0 * NW + wave, last = min(t1 * NW, (seen + kRowsKeys - 1) / kRowsKeys);   // in tiles of 32 keys
     int page = -1;
     if (s0 < last) {
-      kv = key_row(a, lookup(s0), s0 * kRowsKeys + (lane & 31));
+      kv = key_row(a, lookup(s0), s0 * kRowsKeys + (lane & 31), run.len);
       have = (uint32_t)__ballot(kv.ok);
       request_k();
       request_v();
@@ -664,12 +693,10 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
 #pragma unroll
           for (int n = 0; n < NB; ++n) s[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][i], s[n][kb], 0, 0, 0);
         }
-      const bool more = t + NW < last;
-      if (more) {
-        kv = key_row(a, page, (t + NW) * kRowsKeys + (lane & 31));
-        have = (uint32_t)__ballot(kv.ok);
-        request_k();
-      }
+      // (behind the wave's last keys whatever follows, which nothing uses)
+      kv = key_row(a, page, (t + NW) * kRowsKeys + (lane & 31), run.len);
+      have = (uint32_t)__ballot(kv.ok);
+      request_k();
       const bool mask = t >= clear || h != ~0u;
       bool odd = false;
 #pragma unroll
@@ -689,10 +716,8 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
         }
       }
       odd = __any(odd);
-      if (more) {
-        request_v();
-        page = lookup(t + 2 * NW);
-      }
+      request_v();
+      page = lookup(t + 2 * NW);
       uint32_t ph[NB][4], pl[NB][4];
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
