@@ -26,7 +26,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kItemKeys = 128;   // what starting and ending an item costs, in keys
-constexpr int kPartTail = 1, kPartHead = 2, kPartLast = 4;   // flags of a workgroup's unfinished items
+constexpr int kPartTail = 1, kPartHead = 2, kPartLast = 4;   // flags of a workgroup's unfinished items; above them its tail's end
 
 // ---- sharing out ----------------------------------------------------------------------------------------------------
 struct SeqRun {
@@ -45,11 +45,15 @@ __device__ __forceinline__ SeqRun get_run(const RunsArg& r, const PageTableArg& 
   s.len = (int)min((int64_t)max(r.kv_lens[i], 0), (int64_t)pt.per_seq << pt.shift);
   return s;
 }
-// Work of one head of a sequence: block m's is base + slope (m + 1).
+// Work of one head of a sequence, in keys.  Block m's is base + slope (m + 1); the blocks are taken from both ends in turn (last,
+// first, last but one, ...), so that any even number of neighbours is the same work.
 struct SeqCost {
   int64_t base, slope;
   int blocks;
-  __device__ __forceinline__ int64_t before(int64_t m) const { return m * base + slope * (m * (m + 1) / 2); }
+  __device__ __forceinline__ int block(int p) const { return p % 2 ? p / 2 : blocks - 1 - p / 2; }   // the p-th one taken
+  __device__ __forceinline__ int64_t cost(int p) const { return base + slope * (block(p) + 1); }
+  __device__ __forceinline__ int64_t pair() const { return 2 * base + slope * (blocks + 1); }
+  __device__ __forceinline__ int64_t before(int p) const { return p / 2 * pair() + (p % 2 ? cost(p - 1) : 0); }
   __device__ __forceinline__ int64_t head() const { return before(blocks); }
 };
 __device__ __forceinline__ SeqCost get_cost(const SeqRun& s, int tb, int causal) {
@@ -66,14 +70,15 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {   // a value that all 
 }
 
 struct Share {
-  int64_t x0, x1;      // this workgroup's part of the work
-  int w;               // its number
-  bool idle;           // there is no part for it
-  int seq, head, blk;  // the item in which x0 lies,
-  int64_t xs;          // and where that begins
+  int64_t x0, x1;     // this workgroup's part of the work
+  int64_t total;      // all of it
+  int w, n;           // its number, and how many there are
+  bool idle;          // there is no part for it
+  int seq, head, p;   // the item in which x0 lies (the p-th block taken of a head),
+  int64_t xs;         // and where that begins
 };
 
-// NT threads; lds: 2 * NT / 64 + 4 int64 of scratch.
+// NT threads; lds: NT / 64 + 8 int64 of scratch.
 template <int NT>
 __device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* lds) {
   constexpr int NW = NT / kWave;
@@ -83,12 +88,8 @@ __device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* lds)
     const SeqRun s = get_run(a.runs, a.pt, i);
     total += get_cost(s, a.tb, a.causal).head() * a.hkv;
   }
-  auto wave_sum = [](int64_t v) {
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) v += (int64_t)shfl_xor_u64((uint64_t)v, m);
-    return v;
-  };
-  total = wave_sum(total);
+  for (int m = 32; m >= 1; m >>= 1) total += (int64_t)shfl_xor_u64((uint64_t)total, m);
   if (lane == 0) lds[wave] = total;
   __syncthreads();
   total = 0;
@@ -102,13 +103,17 @@ __device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* lds)
   // (n_wg is a multiple of eight, and every number below it is some workgroup's)
   const int per = (n + 7) / 8, x = (int)blockIdx.x % 8, y = (int)blockIdx.x / 8, w = y < per ? x * per + y : 8 * y + x;
   sh.w = w;
+  sh.n = n;
+  sh.total = total;
   sh.idle = w >= n;
   if (sh.idle) return sh;
   const int64_t each = total / n, more = total % n;
-  sh.x0 = each * w + more * w / n;
-  sh.x1 = each * (w + 1) + more * (w + 1) / n;
+  const int64_t cut0 = each * w + more * w / n, cut1 = each * (w + 1) + more * (w + 1) / n;
+  // A cut within `near` keys of an item's end is made there: a split item costs its parts' way through memory.
+  const int64_t near = min(max((int64_t)kItemKeys, each / 32), each / 8);
   int64_t before = 0;   // work of the sequences before the current NT
   int64_t* found = lds + NW;
+  if (tid == 0) found[4] = w + 1 == n ? total : -1;
   for (int i0 = 0; i0 < b; i0 += NT) {
     const int i = i0 + tid;
     SeqCost c{};
@@ -134,36 +139,53 @@ __device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* lds)
       all += lds[k];
     }
     const int64_t from = base + incl - mine;
-    if (mine > 0 && sh.x0 >= from && sh.x0 < from + mine) {
-      const int64_t head = c.head(), h = (sh.x0 - from) / head, rest = (sh.x0 - from) - h * head;
-      // the block: the largest m with before(m) <= rest
-      int64_t m;
-      if (c.slope == 0) {
-        m = rest / c.base;
-      } else {
-        const double p = (double)c.base / (double)c.slope + 0.5;
-        m = (int64_t)(sqrt(p * p + 2.0 * (double)rest / (double)c.slope) - p);
-        m = m < 0 ? 0 : m;
-        while (m > 0 && c.before(m) > rest) --m;
-        while (c.before(m + 1) <= rest) ++m;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int64_t cut = e ? cut1 : cut0;
+      if (mine > 0 && cut >= from && cut < from + mine) {
+        const int64_t head = c.head();
+        int64_t h = (cut - from) / head;
+        const int64_t rest = (cut - from) - h * head;
+        int p = 2 * (int)(rest / c.pair());
+        if (rest - c.before(p) >= c.cost(p)) ++p;
+        const int64_t left = rest - c.before(p), right = c.cost(p) - left;
+        int64_t at = cut;
+        if (left <= near && left <= right) at = cut - left;
+        else if (right <= near) at = cut + right;
+        if (e) {
+          found[4] = at;
+        } else {
+          int s = i;
+          if (at == cut + right && ++p == c.blocks) {   // the item behind
+            p = 0;
+            if (++h == a.hkv) {
+              h = 0;
+              do ++s; while (s < b && get_run(a.runs, a.pt, s).n == 0);
+            }
+          }
+          found[0] = s;
+          found[1] = h;
+          found[2] = p;
+          found[3] = at;
+          found[5] = at == cut ? at - left : at;
+        }
       }
-      found[0] = i;
-      found[1] = h;
-      found[2] = m;
-      found[3] = from + h * head + c.before(m);
     }
     before += all;
   }
   __syncthreads();
   sh.seq = __builtin_amdgcn_readfirstlane((int)found[0]);
   sh.head = __builtin_amdgcn_readfirstlane((int)found[1]);
-  sh.blk = __builtin_amdgcn_readfirstlane((int)found[2]);
-  sh.xs = uniform64(found[3]);
+  sh.p = __builtin_amdgcn_readfirstlane((int)found[2]);
+  sh.x0 = uniform64(found[3]);
+  sh.x1 = uniform64(found[4]);
+  sh.xs = uniform64(found[5]);
+  sh.idle = sh.x0 >= sh.x1;
   __syncthreads();
   return sh;
 }
 
-// The workgroup's items one after the other: work(run, seq, head, blk, first tile, last tile + 1, tiles of the item, part slot or -1).
+// The workgroup's items one after the other: work(run, seq, head, blk, first tile, last tile + 1, part slot or -1).
 template <int NT, int TILE, class F>
 __device__ __forceinline__ void for_items(const PagedAttnArgs& a, int64_t* lds, F&& work) {
   const Share sh = get_share<NT>(a, lds);
@@ -172,17 +194,18 @@ __device__ __forceinline__ void for_items(const PagedAttnArgs& a, int64_t* lds, 
     return;
   }
   int4 desc = make_int4(0, 0, 0, 0);
-  int seq = sh.seq, head = sh.head, blk = sh.blk;
+  int seq = sh.seq, head = sh.head, p = sh.p;
   int64_t xs = sh.xs;
   while (true) {
     const SeqRun run = get_run(a.runs, a.pt, seq);
     const SeqCost c = get_cost(run, a.tb, a.causal);
     while (true) {
-      const int64_t cost = c.base + c.slope * (blk + 1);
+      const int64_t cost = c.cost(p);
+      const int blk = c.block(p);
       const int seen = a.causal ? min(max(run.len - run.n + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
       const int tiles = (seen + TILE - 1) / TILE;
-      auto tile_at = [&](int64_t p) {
-        return p >= cost ? tiles : p <= kItemKeys ? 0 : (int)min((int64_t)tiles, (p - kItemKeys) / TILE);
+      auto tile_at = [&](int64_t x) {
+        return x >= cost ? tiles : x <= kItemKeys ? 0 : (int)min((int64_t)tiles, (x - kItemKeys) / TILE);
       };
       const int t0 = tile_at(sh.x0 - xs), t1 = tile_at(sh.x1 - xs);
       if (t0 < t1 || (tiles == 0 && xs >= sh.x0)) {
@@ -192,7 +215,9 @@ __device__ __forceinline__ void for_items(const PagedAttnArgs& a, int64_t* lds, 
           desc.x |= kPartHead | (t1 == tiles ? kPartLast : 0);
         } else if (t1 < tiles) {
           slot = 2 * sh.w + 1;
-          desc = make_int4(desc.x | kPartTail, seq, head, blk);
+          // the workgroup that the item's end lies in, or one next to it: cuts lie no further than an eighth of a share from their place
+          const int end = min(sh.n - 1, (int)((double)(xs + cost - 1) * sh.n / (double)sh.total));
+          desc = make_int4((desc.x & 7) | kPartTail | end << 3, seq, head, blk);
         }
         work(run, seq, head, blk, t0, t1, slot);
       }
@@ -201,8 +226,8 @@ __device__ __forceinline__ void for_items(const PagedAttnArgs& a, int64_t* lds, 
         if (threadIdx.x == 0) a.desc[sh.w] = desc;
         return;
       }
-      if (++blk == c.blocks) {
-        blk = 0;
+      if (++p == c.blocks) {
+        p = 0;
         if (++head == a.hkv) break;
       }
     }
@@ -298,7 +323,7 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
   constexpr bool kEven = kTileKeys * kPieces % kTileNT == 0;
   constexpr int PK = TilePitch<D>::k, PV = TilePitch<D>::v, QS = D / 16, DB = D / 32;
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * TilePitch<D>::bytes];
-  __shared__ int64_t scratch[2 * kTileNT / kWave + 4];
+  __shared__ int64_t scratch[kTileNT / kWave + 8];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, col = lane & 31, half = lane >> 5;
   // this thread's pieces of a tile: piece pc of rows pr + j kRowStep (a row's pieces lie on neighbouring threads)
   const int pr = tid / kPieces, pc = tid - pr * kPieces;
@@ -469,6 +494,16 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int j = 0; j < 16; ++j) top = fmaxf(top, s[kb][j]);
+      const uint8_t* vp = buf + kTileKeys * PK + (4 * half + ((lane & 15) >> 2)) * PV + (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+      uint4 vf[2][DB];
+      auto read_values = [&](int u, uint4 (&f)[DB]) {   // 16 keys
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+          const uint2 x = read_tr(vp + u * 16 * PV + i * 64), y = read_tr(vp + (u * 16 + 8) * PV + i * 64);
+          f[i] = make_uint4(x.x, x.y, y.x, y.y);
+        }
+      };
+      read_values(0, vf[0]);   // arrives while the weights are formed
       top = max_halves(top) * a.scale_log2;
       // The maximum follows the logits only where they pass it by 2^8: weights up to that lose nothing in bf16 or in fp32 sums.
       if (__any(top > m + 8.f)) {
@@ -483,15 +518,13 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
       const float mm = m == -INFINITY ? 0.f : m;
       uint32_t pw[2][8];
       float sum = 0.f;
+      auto weigh = [&](int kb, int c) {   // two keys
+        const float p0 = __builtin_amdgcn_exp2f(s[kb][2 * c] * a.scale_log2 - mm), p1 = __builtin_amdgcn_exp2f(s[kb][2 * c + 1] * a.scale_log2 - mm);
+        sum += p0 + p1;
+        pw[kb][c] = pack_bf16(p0, p1);
+      };
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int j = 0; j < 16; j += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(s[kb][j] * a.scale_log2 - mm), p1 = __builtin_amdgcn_exp2f(s[kb][j + 1] * a.scale_log2 - mm);
-          sum += p0 + p1;
-          pw[kb][j >> 1] = pack_bf16(p0, p1);
-        }
-      l += sum;
+      for (int c = 0; c < 8; ++c) weigh(0, c);
       uint8_t* vt = buf + kTileKeys * PK;
       if (odd) {
         // infinities and NaN go to the rows that see their keys, and are zero for the product
@@ -516,26 +549,29 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
         __syncthreads();
       }
       {
-        const uint8_t* vp = vt + (4 * half + ((lane & 15) >> 2)) * PV + (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
-        uint4 vf[2][DB];
-        auto read = [&](int u, uint4 (&f)[DB]) {   // 16 keys
-#pragma unroll
-          for (int i = 0; i < DB; ++i) {
-            const uint2 x = read_tr(vp + u * 16 * PV + i * 64), y = read_tr(vp + (u * 16 + 8) * PV + i * 64);
-            f[i] = make_uint4(x.x, x.y, y.x, y.y);
-          }
-        };
-        read(0, vf[0]);
+        if (odd) read_values(0, vf[0]);   // (they were read before they were cleaned)
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          if (u < 3) read(u + 1, vf[(u + 1) % 2]);
+          if (u < 3) read_values(u + 1, vf[(u + 1) % 2]);
           __builtin_amdgcn_sched_barrier(0);
           const uint32_t* p = pw[u / 2] + 4 * (u % 2);
           const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(p[0], p[1], p[2], p[3]));
 #pragma unroll
-          for (int i = 0; i < DB; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[u % 2][i]), pf, o[i], 0, 0, 0);
+          for (int i = 0; i < DB; ++i) {
+            o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[u % 2][i]), pf, o[i], 0, 0, 0);
+            // the weights of the second 32 keys beside the products of the first
+            if (u < 2) {
+#pragma unroll
+              for (int c = 8 * (u * DB + i) / (2 * DB); c < 8 * (u * DB + i + 1) / (2 * DB); ++c) {
+                weigh(1, c);
+                asm volatile("" : "+v"(pw[1][c]), "+v"(sum));   // (keeps them here)
+              }
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
+        l += sum;
       }
       mask = t + 1 < t1 && masked(t + 1);
       bool bad = false;
@@ -588,7 +624,7 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
   constexpr int PV = RowsPitch<D>::v;
   constexpr int kVBytes = NW * kRowsKeys * PV, kMergeBytes = NW * BR * (D * 4 + 8);
   __shared__ __attribute__((aligned(16))) uint8_t lds[kVBytes > kMergeBytes ? kVBytes : kMergeBytes];
-  __shared__ int64_t scratch[2 * kRowsNT / kWave + 4];
+  __shared__ int64_t scratch[kRowsNT / kWave + 8];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, col = lane & 15, quarter = lane >> 4;
 
   for_items<kRowsNT, kRowsKeys * NW>(a, scratch, [&](const SeqRun& run, int seq, int head, int blk, int t0, int t1, int slot) {
