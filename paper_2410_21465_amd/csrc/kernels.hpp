@@ -248,7 +248,7 @@ struct PagedAttnArgs {
   int tb;                   // tokens per row block
   int n_wg;                 // workgroups the work is shared out to at most
   int min_share;            // least work of a workgroup, in keys
-  int4* desc;               // [n_wg] {flags, sequence, KV head, row block} of the items that a workgroup leaves unfinished
+  int4* desc;               // [n_wg] flags of the items that a workgroup leaves unfinished; of its last one first token, KV head and rows
   float* part_acc;          // [2 n_wg, block rows, d] unnormalised sums
   float2* part_ml;          // [2 n_wg, block rows] (max in log2 units, sum)
 };

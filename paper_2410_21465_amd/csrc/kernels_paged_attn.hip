@@ -6,96 +6,134 @@ namespace skv {
 
 // Joins the parts of the items that are left unfinished, in ascending order: workgroup w of the first kernel began one
 // (kPartTail, slot 2 w + 1), the workgroups behind it went on with it (kPartHead, slots 2 w') up to the one that finished it
-// (kPartLast).  Groups of 32 threads, each with the columns of a row.  GROUPED (16 or 32 rows and up to hundreds of parts of a long
-// cache): eight groups share the parts of one row; otherwise 32 groups have a row each and go through the block's rows.
-template <bool GROUPED>
-__global__ __launch_bounds__(GROUPED ? 256 : 1024) void paged_attn_join_kernel(PagedAttnArgs a, int block_rows) {
-  const int w = blockIdx.x, tid = threadIdx.x, grp = tid >> 5, c = (tid & 31) * 4;
-  const int4 desc = a.desc[w];
-  if (!(desc.x & kPartTail)) return;
-  const SeqRun run = get_run(a.runs, a.pt, desc.y);
-  float m, l, x[4];
-  int row, tl, g, tok;
-  bool ok;
-  auto start = [&](int r) {
-    row = r;
-    tl = row / a.G;
-    g = row - tl * a.G;
-    tok = desc.w * a.tb + tl;
-    ok = tl < a.tb && tok < run.n && c < a.d;
-    m = -INFINITY;
-    l = x[0] = x[1] = x[2] = x[3] = 0.f;
-  };
-  auto add = [&](const float2 ml, const float4 v) {
+// (kPartLast).  Groups of 32 threads, each with the columns of a row.
+struct Joined {   // a row's state as parts are added
+  float m = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void add(const float2 ml, const float4 v) {
     if (ml.x == -INFINITY && ml.y == 0.f) return;
     const float top = fmaxf(m, ml.x);
     const float fo = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), fn = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
     m = top;
     l = l * fo + ml.y * fn;
     x[0] = x[0] * fo + v.x * fn; x[1] = x[1] * fo + v.y * fn; x[2] = x[2] * fo + v.z * fn; x[3] = x[3] * fo + v.w * fn;
-  };
-  auto part = [&](int64_t slot) {
-    add(a.part_ml[slot * block_rows + row], *reinterpret_cast<const float4*>(a.part_acc + (slot * block_rows + row) * a.d + c));
-  };
-  auto finish = [&]() {
+  }
+  __device__ __forceinline__ void finish(const PagedAttnArgs& a, int64_t qrow, int h, int c) const {
     const float f = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-    const int64_t qrow = run.start + tok;
-    const int h = desc.z * a.G + g;
     *reinterpret_cast<uint2*>(a.out.p + qrow * a.out.tok + h * a.out.head + c * 2) =
         make_uint2(pack_bf16(x[0] * f, x[1] * f), pack_bf16(x[2] * f, x[3] * f));
     if (a.lse && c == 0) a.lse[qrow * a.hq + h] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+};
+
+// 128 rows, two or three parts: workgroup w joins the item that its like began, a row per group at a time.
+__global__ __launch_bounds__(1024) void paged_attn_join_blocks_kernel(PagedAttnArgs a, int block_rows) {
+  const int w = blockIdx.x, c = ((int)threadIdx.x & 31) * 4;
+  const int4 desc = a.desc[w];
+  if (!(desc.x & kPartTail) || c >= a.d) return;
+  for (int row = threadIdx.x >> 5; row < desc.w; row += 32) {
+    const int tl = row / a.G, g = row - tl * a.G;
+    Joined j;
+    auto part = [&](int64_t slot) {
+      j.add(a.part_ml[slot * block_rows + row], *reinterpret_cast<const float4*>(a.part_acc + (slot * block_rows + row) * a.d + c));
+    };
+    part(2 * (int64_t)w + 1);
+    for (int i = w + 1; i < a.n_wg; ++i) {
+      const int f = a.desc[i].x;
+      if (f & kPartHead) part(2 * (int64_t)i);
+      if (f & kPartLast) break;
+    }
+    j.finish(a, (int64_t)desc.y + tl, desc.z * a.G + g, c);
+  }
+}
+
+// 16 or 32 rows and up to hundreds of parts.  All is latency: one load and a vote find the parts, eight of them are requested at a time.
+// Up to kFewParts of them are joined where the item began, each of the 16 groups with a row of its own; the rows of an item with
+// more are shared by the workgroups whose like worked at it, and the 16 groups share the parts of a row.
+constexpr int kFewParts = 16;
+__global__ __launch_bounds__(512) void paged_attn_join_rows_kernel(PagedAttnArgs a, int block_rows) {
+  constexpr int kGroups = 16, kAhead = 8, kWords = 512 / kWave;
+  __shared__ float acc_s[kGroups][128];
+  __shared__ float2 ml_s[kGroups];
+  __shared__ uint64_t tails[kWords], heads[kWords], lasts[kWords];
+  const int me = blockIdx.x, tid = threadIdx.x, grp = tid >> 5, c = (tid & 31) * 4, col = min(c, a.d - 4);
+  const int flags = tid < a.n_wg ? a.desc[tid].x : 0;
+  const int4 mine = a.desc[me];
+  {
+    const uint64_t t = __ballot(flags & kPartTail), h = __ballot(flags & kPartHead), l = __ballot(flags & kPartLast);
+    if (tid % kWave == 0) { tails[tid / kWave] = t; heads[tid / kWave] = h; lasts[tid / kWave] = l; }
+  }
+  __syncthreads();
+  auto end_of = [&](int w) {   // the first behind w that finished an item
+    uint64_t m = w % 64 == 63 ? 0 : lasts[w / 64] >> (w % 64 + 1) << (w % 64 + 1);
+    int i = w / 64;
+    while (m == 0 && ++i < kWords) m = lasts[i];
+    return m ? i * 64 + __ffsll((unsigned long long)m) - 1 : a.n_wg - 1;
   };
-  if constexpr (!GROUPED) {
-    for (int r = grp; r < a.tb * a.G; r += 32) {
-      start(r);
-      if (!ok) continue;
-      part(2 * (int64_t)w + 1);
-      for (int i = w + 1; i < a.n_wg; ++i) {
-        const int f = a.desc[i].x;
-        if (f & kPartHead) part(2 * (int64_t)i);
-        if (f & kPartLast) break;
-      }
-      finish();
-    }
-  } else {
-    __shared__ float acc_s[8][128];
-    __shared__ float2 ml_s[8];
-    __shared__ int end_s;
-    if (tid == 0) end_s = a.n_wg;
-    __syncthreads();
-    // the first that finished an item is the one that finished this
-    for (int i = w + 1 + tid; i <= min((desc.x >> 3) + 1, a.n_wg - 1); i += 256)
-      if (a.desc[i].x & kPartLast) atomicMin(&end_s, i);
-    __syncthreads();
-    const int end = min(end_s, a.n_wg - 1);
-    start((int)blockIdx.y);
-    if (tl >= a.tb || tok >= run.n) return;
-    if (ok) {
-#pragma unroll 4
-      for (int i = w + grp; i <= end; i += 8)
-        if (i == w) part(2 * (int64_t)w + 1);
-        else if (a.desc[i].x & kPartHead) part(2 * (int64_t)i);
-    }
-    if (c < a.d) *reinterpret_cast<float4*>(&acc_s[grp][c]) = make_float4(x[0], x[1], x[2], x[3]);
-    if (c == 0) ml_s[grp] = make_float2(m, l);
-    __syncthreads();
-    if (grp > 0 || c >= a.d) return;
-    m = -INFINITY;
-    l = x[0] = x[1] = x[2] = x[3] = 0.f;
+  auto begin_of = [&](int w) {   // the last before w that began one, -1: none
+    uint64_t m = tails[w / 64] & ((1ull << (w % 64)) - 1);
+    int i = w / 64;
+    while (m == 0 && --i >= 0) m = tails[i];
+    return m ? i * 64 + 63 - __clzll((long long)m) : -1;
+  };
+  for (int e = 0; e < 2; ++e) {   // what began here, and what lies around this workgroup's part, if any
+    const int w = e ? begin_of(me) : (mine.x & kPartTail ? me : -1);
+    if (w < 0) continue;
+    const int end = end_of(w), parts = end - w + 1;
+    if (e && (end < me || parts <= kFewParts)) continue;
+    const int4 desc = e ? a.desc[w] : mine;
+    // parts first, first + step, ... of a row
+    auto gather = [&](int row, int first, int step) {
+      Joined j;
+      for (int i0 = first; i0 < parts; i0 += step * kAhead) {
+        float2 ml[kAhead];
+        float4 v[kAhead];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) add(ml_s[i], *reinterpret_cast<const float4*>(&acc_s[i][c]));
-    finish();
+        for (int k = 0; k < kAhead; ++k) {   // (places in the workspace, whatever they hold)
+          const int i = min(i0 + k * step, parts - 1);
+          const int64_t slot = (2 * (int64_t)(w + i) + (i == 0 ? 1 : 0)) * block_rows + row;
+          ml[k] = a.part_ml[slot];
+          v[k] = *reinterpret_cast<const float4*>(a.part_acc + slot * a.d + col);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int i = i0 + k * step;   // (workgroups inside that had less than a tile to do have no part)
+          if (i < parts && (i == 0 || (heads[(w + i) / 64] >> ((w + i) % 64) & 1))) j.add(ml[k], v[k]);
+        }
+      }
+      return j;
+    };
+    auto finish = [&](const Joined& j, int row) {
+      const int tl = row / a.G;
+      if (c < a.d) j.finish(a, (int64_t)desc.y + tl, desc.z * a.G + row - tl * a.G, c);
+    };
+    if (parts <= kFewParts) {
+      for (int row = grp; row < desc.w; row += kGroups) finish(gather(row, 0, 1), row);
+      continue;
+    }
+    for (int row = me - w; row < desc.w; row += parts) {
+      const Joined j = gather(row, grp, kGroups);
+      __syncthreads();   // (the row before)
+      if (c < a.d) *reinterpret_cast<float4*>(&acc_s[grp][c]) = make_float4(j.x[0], j.x[1], j.x[2], j.x[3]);
+      if (c == 0) ml_s[grp] = make_float2(j.m, j.l);
+      __syncthreads();
+      if (grp == 0) {
+        Joined all;
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) all.add(ml_s[i], *reinterpret_cast<const float4*>(&acc_s[i][col]));
+        finish(all, row);
+      }
+    }
   }
 }
 
 int paged_attn_block_rows(int G, long rows) { return G <= 16 && rows <= 16 ? 16 : G <= 32 && rows <= 32 ? 32 : kTileRows; }
-int paged_attn_workgroups(int block_rows) { return 512; }   // two per compute unit
+int paged_attn_workgroups(int block_rows) { return 512; }   // two per compute unit; a multiple of eight, and at most 512 (the join)
 
 hipError_t launch_paged_attention(PagedAttnArgs a, int block_rows, hipStream_t st) {
   hipError_t e = a.kv_bytes == 1 ? launch_paged_attn_fp8(a, block_rows, st) : launch_paged_attn_eb<2>(a, block_rows, st);
   if (e != hipSuccess) return e;
-  if (block_rows == kTileRows) hipLaunchKernelGGL(paged_attn_join_kernel<false>, dim3(a.n_wg), dim3(1024), 0, st, a, block_rows);
-  else hipLaunchKernelGGL(paged_attn_join_kernel<true>, dim3(a.n_wg, a.tb * a.G), dim3(256), 0, st, a, block_rows);
+  if (block_rows == kTileRows) hipLaunchKernelGGL(paged_attn_join_blocks_kernel, dim3(a.n_wg), dim3(1024), 0, st, a, block_rows);
+  else hipLaunchKernelGGL(paged_attn_join_rows_kernel, dim3(a.n_wg), dim3(512), 0, st, a, block_rows);
   return hipGetLastError();
 }
 

@@ -26,7 +26,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kItemKeys = 128;   // what starting and ending an item costs, in keys
-constexpr int kPartTail = 1, kPartHead = 2, kPartLast = 4;   // flags of a workgroup's unfinished items; above them its tail's end
+constexpr int kPartTail = 1, kPartHead = 2, kPartLast = 4;   // flags of a workgroup's unfinished items
 
 // ---- sharing out ----------------------------------------------------------------------------------------------------
 struct SeqRun {
@@ -71,82 +71,79 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {   // a value that all 
 
 struct Share {
   int64_t x0, x1;     // this workgroup's part of the work
-  int64_t total;      // all of it
-  int w, n;           // its number, and how many there are
+  int w;              // its number
   bool idle;          // there is no part for it
   int seq, head, p;   // the item in which x0 lies (the p-th block taken of a head),
   int64_t xs;         // and where that begins
 };
 
-// NT threads; lds: NT / 64 + 8 int64 of scratch.
-template <int NT>
-__device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* lds) {
-  constexpr int NW = NT / kWave;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, b = a.runs.batch;
-  int64_t total = 0;
-  for (int i = tid; i < b; i += NT) {
-    const SeqRun s = get_run(a.runs, a.pt, i);
-    total += get_cost(s, a.tb, a.causal).head() * a.hkv;
+// a / b for 0 <= a < 2^52, b > 0, through fp64: the quotient is off by one at most before it is put right (the compiler's 64-bit
+// division is some hundred instructions)
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  int64_t q = (int64_t)((double)a * (1.0 / (double)b));
+  const int64_t r = a - q * b;
+  if (r < 0) --q;
+  if (r >= b) ++q;
+  return q;
+}
+// inclusive sum over the wave's lanes, as wave_incl_scan_u32
+__device__ __forceinline__ int64_t dpp_add_i64(int64_t x, int lo, int hi) { return x + (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo); }
+__device__ __forceinline__ int64_t wave_scan_i64(int64_t x) {
+#define SKV_STEP(CTRL, MASK)                                                                        \
+  x = dpp_add_i64(x, __builtin_amdgcn_update_dpp(0, (int)x, CTRL, MASK, 0xf, false),                \
+                  __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, MASK, 0xf, false));
+  SKV_STEP(0x111, 0xf) SKV_STEP(0x112, 0xf) SKV_STEP(0x114, 0xf) SKV_STEP(0x118, 0xf) SKV_STEP(0x142, 0xa) SKV_STEP(0x143, 0xc)
+#undef SKV_STEP
+  return x;
+}
+__device__ __forceinline__ int64_t last_lane_i64(int64_t x) {
+  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), kWave - 1) << 32) |
+                   (uint32_t)__builtin_amdgcn_readlane((int)x, kWave - 1));
+}
+
+// Every wave for itself, 64 sequences at a time; found: 8 int64 of LDS of its own.
+__device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* found) {
+  const int lane = threadIdx.x & (kWave - 1), b = a.runs.batch;
+  auto cost_of = [&](int i, SeqCost& c) {
+    c = get_cost(get_run(a.runs, a.pt, min(i, b - 1)), a.tb, a.causal);
+    return i < b ? c.head() * a.hkv : 0;
+  };
+  SeqCost c;
+  int64_t incl = wave_scan_i64(cost_of(lane, c)), total = last_lane_i64(incl);   // of the first 64
+  for (int i0 = kWave; i0 < b; i0 += kWave) {
+    SeqCost d;
+    total += last_lane_i64(wave_scan_i64(cost_of(i0 + lane, d)));
   }
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) total += (int64_t)shfl_xor_u64((uint64_t)total, m);
-  if (lane == 0) lds[wave] = total;
-  __syncthreads();
-  total = 0;
-#pragma unroll
-  for (int i = 0; i < NW; ++i) total += lds[i];
-  total = uniform64(total);
   Share sh;
-  const int64_t n64 = (total + a.min_share - 1) / a.min_share;
+  const int64_t n64 = quotient(total + a.min_share - 1, a.min_share);
   const int n = (int)(n64 < a.n_wg ? n64 : a.n_wg);
   // neighbouring shares to one XCD (workgroups go round the eight of them), whose L2 then holds a head's K and V for all
   // (n_wg is a multiple of eight, and every number below it is some workgroup's)
   const int per = (n + 7) / 8, x = (int)blockIdx.x % 8, y = (int)blockIdx.x / 8, w = y < per ? x * per + y : 8 * y + x;
   sh.w = w;
-  sh.n = n;
-  sh.total = total;
   sh.idle = w >= n;
   if (sh.idle) return sh;
-  const int64_t each = total / n, more = total % n;
+  const int64_t each = quotient(total, n);
+  const int more = (int)(total - each * n);   // (below n, and n below 2^11)
   const int64_t cut0 = each * w + more * w / n, cut1 = each * (w + 1) + more * (w + 1) / n;
   // A cut within `near` keys of an item's end is made there: a split item costs its parts' way through memory.
   const int64_t near = min(max((int64_t)kItemKeys, each / 32), each / 8);
-  int64_t before = 0;   // work of the sequences before the current NT
-  int64_t* found = lds + NW;
-  if (tid == 0) found[4] = w + 1 == n ? total : -1;
-  for (int i0 = 0; i0 < b; i0 += NT) {
-    const int i = i0 + tid;
-    SeqCost c{};
-    int64_t mine = 0;
-    if (i < b) {
-      c = get_cost(get_run(a.runs, a.pt, i), a.tb, a.causal);
-      mine = c.head() * a.hkv;
+  int64_t before = 0;   // work of the sequences before these 64
+  if (lane == 0) found[4] = w + 1 == n ? total : -1;
+  for (int i0 = 0; i0 < b; i0 += kWave) {
+    if (i0 > 0) {
+      before += last_lane_i64(incl);
+      incl = wave_scan_i64(cost_of(i0 + lane, c));
     }
-    int64_t incl = mine;
-#pragma unroll
-    for (int m = 1; m < kWave; m <<= 1) {
-      const int64_t up = (int64_t)(((uint64_t)(uint32_t)__shfl_up((int)(incl >> 32), m, kWave) << 32) |
-                                   (uint32_t)__shfl_up((int)incl, m, kWave));
-      if (lane >= m) incl += up;
-    }
-    __syncthreads();
-    if (lane == kWave - 1) lds[wave] = incl;
-    __syncthreads();
-    int64_t base = before, all = 0;
-#pragma unroll
-    for (int k = 0; k < NW; ++k) {
-      if (k < wave) base += lds[k];
-      all += lds[k];
-    }
-    const int64_t from = base + incl - mine;
+    const int64_t mine = i0 + lane < b ? c.head() * a.hkv : 0, from = before + incl - mine;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int64_t cut = e ? cut1 : cut0;
       if (mine > 0 && cut >= from && cut < from + mine) {
         const int64_t head = c.head();
-        int64_t h = (cut - from) / head;
+        int64_t h = quotient(cut - from, head);
         const int64_t rest = (cut - from) - h * head;
-        int p = 2 * (int)(rest / c.pair());
+        int p = 2 * (int)quotient(rest, c.pair());
         if (rest - c.before(p) >= c.cost(p)) ++p;
         const int64_t left = rest - c.before(p), right = c.cost(p) - left;
         int64_t at = cut;
@@ -155,7 +152,7 @@ __device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* lds)
         if (e) {
           found[4] = at;
         } else {
-          int s = i;
+          int s = i0 + lane;
           if (at == cut + right && ++p == c.blocks) {   // the item behind
             p = 0;
             if (++h == a.hkv) {
@@ -171,9 +168,9 @@ __device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* lds)
         }
       }
     }
-    before += all;
   }
-  __syncthreads();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (written by one lane, read by all)
+  __builtin_amdgcn_wave_barrier();
   sh.seq = __builtin_amdgcn_readfirstlane((int)found[0]);
   sh.head = __builtin_amdgcn_readfirstlane((int)found[1]);
   sh.p = __builtin_amdgcn_readfirstlane((int)found[2]);
@@ -181,58 +178,77 @@ __device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* lds)
   sh.x1 = uniform64(found[4]);
   sh.xs = uniform64(found[5]);
   sh.idle = sh.x0 >= sh.x1;
-  __syncthreads();
   return sh;
 }
 
-// The workgroup's items one after the other: work(run, seq, head, blk, first tile, last tile + 1, part slot or -1).
-template <int NT, int TILE, class F>
-__device__ __forceinline__ void for_items(const PagedAttnArgs& a, int64_t* lds, F&& work) {
-  const Share sh = get_share<NT>(a, lds);
-  if (sh.idle) {   // every entry of desc is written by every call
-    if (threadIdx.x == 0) a.desc[sh.w] = make_int4(0, 0, 0, 0);
-    return;
+// The workgroup's items one after the other: work(run, seq, head, blk, first tile, last tile + 1, part slot or -1).  What is only wanted
+// between items waits in LDS (a copy per wave): in scalar registers it made the loops over keys spill theirs.
+template <int TILE, class F>
+__device__ __forceinline__ void for_items(const PagedAttnArgs& a, F&& work) {
+  struct State {
+    int64_t x0, x1, xs;
+    int w, seq, head, p, done;
+    int4 desc;
+  };
+  __shared__ int64_t found[4][8];   // (256 threads)
+  __shared__ State state[4];
+  State& st = state[threadIdx.x / kWave];
+  {
+    const Share sh = get_share(a, found[threadIdx.x / kWave]);
+    if (sh.idle) {   // every entry of desc is written by every call
+      if (threadIdx.x == 0) a.desc[sh.w] = make_int4(0, 0, 0, 0);
+      return;
+    }
+    st.x0 = sh.x0; st.x1 = sh.x1; st.xs = sh.xs;
+    st.w = sh.w; st.seq = sh.seq; st.head = sh.head; st.p = sh.p; st.done = 0;
+    st.desc = make_int4(0, 0, 0, 0);
   }
-  int4 desc = make_int4(0, 0, 0, 0);
-  int seq = sh.seq, head = sh.head, p = sh.p;
-  int64_t xs = sh.xs;
+  auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
   while (true) {
+    asm volatile("" ::: "memory");
+    if (uniform(st.done)) break;
+    const int seq = uniform(st.seq), head = uniform(st.head), p = uniform(st.p), w = uniform(st.w);
+    const int64_t xs = uniform64(st.xs), x0 = uniform64(st.x0), x1 = uniform64(st.x1);
     const SeqRun run = get_run(a.runs, a.pt, seq);
     const SeqCost c = get_cost(run, a.tb, a.causal);
-    while (true) {
-      const int64_t cost = c.cost(p);
-      const int blk = c.block(p);
-      const int seen = a.causal ? min(max(run.len - run.n + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
-      const int tiles = (seen + TILE - 1) / TILE;
-      auto tile_at = [&](int64_t x) {
-        return x >= cost ? tiles : x <= kItemKeys ? 0 : (int)min((int64_t)tiles, (x - kItemKeys) / TILE);
-      };
-      const int t0 = tile_at(sh.x0 - xs), t1 = tile_at(sh.x1 - xs);
-      if (t0 < t1 || (tiles == 0 && xs >= sh.x0)) {
-        int slot = -1;
-        if (t0 > 0) {
-          slot = 2 * sh.w;
-          desc.x |= kPartHead | (t1 == tiles ? kPartLast : 0);
-        } else if (t1 < tiles) {
-          slot = 2 * sh.w + 1;
-          // the workgroup that the item's end lies in, or one next to it: cuts lie no further than an eighth of a share from their place
-          const int end = min(sh.n - 1, (int)((double)(xs + cost - 1) * sh.n / (double)sh.total));
-          desc = make_int4((desc.x & 7) | kPartTail | end << 3, seq, head, blk);
-        }
-        work(run, seq, head, blk, t0, t1, slot);
-      }
-      xs += cost;
-      if (xs >= sh.x1) {
-        if (threadIdx.x == 0) a.desc[sh.w] = desc;
-        return;
-      }
-      if (++p == c.blocks) {
-        p = 0;
-        if (++head == a.hkv) break;
+    const int64_t cost = c.cost(p);
+    const int blk = c.block(p);
+    const int seen = a.causal ? min(max(run.len - run.n + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
+    const int tiles = (seen + TILE - 1) / TILE;
+    auto tile_at = [&](int64_t x) {
+      return x >= cost ? tiles : x <= kItemKeys ? 0 : (int)min((int64_t)tiles, (x - kItemKeys) / TILE);
+    };
+    const int t0 = tile_at(x0 - xs), t1 = tile_at(x1 - xs);
+    const bool some = t0 < t1 || (tiles == 0 && xs >= x0);
+    int slot = -1;
+    if (some) {
+      if (t0 > 0) {
+        slot = 2 * w;
+        st.desc.x |= kPartHead | (t1 == tiles ? kPartLast : 0);
+      } else if (t1 < tiles) {
+        slot = 2 * w + 1;
+        st.desc = make_int4(uniform(st.desc.x) | kPartTail, run.start + blk * a.tb, head, min(a.tb, run.n - blk * a.tb) * a.G);
       }
     }
-    head = 0;
-    do ++seq; while (get_run(a.runs, a.pt, seq).n == 0);   // (xs < x1: there is one)
+    st.xs = xs + cost;
+    if (xs + cost >= x1) {
+      st.done = 1;
+      if (threadIdx.x == 0) a.desc[w] = st.desc;
+    } else if (p + 1 < c.blocks) {
+      st.p = p + 1;
+    } else {
+      st.p = 0;
+      if (head + 1 < a.hkv) {
+        st.head = head + 1;
+      } else {
+        st.head = 0;
+        int s = seq;
+        do ++s; while (get_run(a.runs, a.pt, s).n == 0);   // (xs < x1: there is one)
+        st.seq = s;
+      }
+    }
+    asm volatile("" ::: "memory");
+    if (some) work(run, seq, head, blk, t0, t1, slot);
   }
 }
 
@@ -290,7 +306,7 @@ struct KeyRow {
 };
 // (always a load, of the last token's entry for keys behind it: whether the key has a row is asked when the entry is used)
 __device__ __forceinline__ int page_entry(const PagedAttnArgs& a, const int32_t* table, int key, int len) {
-  return table[min(key, len - 1) >> a.pt.shift];
+  return table[min(key, max(len - 1, 0)) >> a.pt.shift];
 }
 __device__ __forceinline__ KeyRow key_row(const PagedAttnArgs& a, int page, int key, int len) {
   KeyRow r;
@@ -323,12 +339,11 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
   constexpr bool kEven = kTileKeys * kPieces % kTileNT == 0;
   constexpr int PK = TilePitch<D>::k, PV = TilePitch<D>::v, QS = D / 16, DB = D / 32;
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * TilePitch<D>::bytes];
-  __shared__ int64_t scratch[kTileNT / kWave + 8];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, col = lane & 31, half = lane >> 5;
   // this thread's pieces of a tile: piece pc of rows pr + j kRowStep (a row's pieces lie on neighbouring threads)
   const int pr = tid / kPieces, pc = tid - pr * kPieces;
 
-  for_items<kTileNT, kTileKeys>(a, scratch, [&](const SeqRun& run, int seq, int head, int blk, int t0, int t1, int slot) {
+  for_items<kTileKeys>(a, [&](const SeqRun& run, int seq, int head, int blk, int t0, int t1, int slot) {
     const int G = a.G, row = wave * 32 + col, tl = row / G, g = row - tl * G, tok = blk * a.tb + tl;
     const bool row_ok = tl < a.tb && tok < run.n;
     const int limit = row_ok ? (a.causal ? run.len - run.n + tok : run.len - 1) : -1;   // last key the row sees
@@ -337,14 +352,16 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
     const int64_t qrow = run.start + tok;
     bf16x8 qf[QS];
     {
+      // (rows that are none take row 0 of q: what they make is not written)
       const uint8_t* qp = a.q.p + (row_ok ? qrow * a.q.tok + (head * G + g) * a.q.head : 0) + half * 16;
 #pragma unroll
       for (int s = 0; s < QS; ++s) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (row_ok) w = *reinterpret_cast<const uint4*>(qp + s * 32);
-        qf[s] = __builtin_bit_cast(bf16x8, w);
+        qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + s * 32));
       }
     }
+    // (waited for here: left to the loop's first products, every turn of it would wait as long)
+#pragma unroll
+    for (int i = 0; i < QS; ++i) asm volatile("" : "+v"(qf[i]));
     f32x16 o[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i)
@@ -635,10 +652,12 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
   constexpr int PV = RowsPitch<D>::v;
   constexpr int kVBytes = NW * kRowsKeys * PV, kMergeBytes = NW * BR * (D * 4 + 8);
   __shared__ __attribute__((aligned(16))) uint8_t lds[kVBytes > kMergeBytes ? kVBytes : kMergeBytes];
-  __shared__ int64_t scratch[kRowsNT / kWave + 8];
+  // Q of two row blocks waits in LDS, in operand order: with it in registers heads of 128 spilled 54 of theirs
+  constexpr bool kQInLds = NB == 2;
+  __shared__ uint4 q_lds[kQInLds ? NB * kSteps : 1][kWave];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, col = lane & 15, quarter = lane >> 4;
 
-  for_items<kRowsNT, kRowsKeys * NW>(a, scratch, [&](const SeqRun& run, int seq, int head, int blk, int t0, int t1, int slot) {
+  for_items<kRowsKeys * NW>(a, [&](const SeqRun& run, int seq, int head, int blk, int t0, int t1, int slot) {
     const int G = a.G;
     // Element order of step s: bf16, 32 s + 8 quarter + 0..7; FP8, whose 16-byte pieces hold 16 elements, steps 2 p and 2 p + 1
     // take the halves of piece 64 p + 16 quarter (a last odd step 8-byte pieces).
@@ -646,21 +665,31 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
       if (EB == 2 || (s == kSteps - 1 && kSteps % 2)) return 32 * s + 8 * quarter;
       return 64 * (s / 2) + 16 * quarter + 8 * (s % 2);
     };
-    bf16x8 qf[NB][kSteps];
+    const int32_t* table = a.pt.table + seq * a.pt.stride;
+    const int seen = a.causal ? min(max(run.len - run.n + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
+    const int s0 = t0 * NW + wave, last = min(t1 * NW, (seen + kRowsKeys - 1) / kRowsKeys);   // in tiles of 32 keys
+    auto lookup = [&](int t) { return page_entry(a, table, t * kRowsKeys + (lane & 31), run.len); };
+    const int page0 = lookup(s0);
+    int page = lookup(s0 + NW);   // of the tile after next
+    bf16x8 qf[kQInLds ? 1 : NB][kSteps];
     int limit[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const int row = 16 * n + col, tl = row / G, g = row - tl * G, tok = blk * a.tb + tl;
       const bool ok = tl < a.tb && tok < run.n;
       limit[n] = ok ? (a.causal ? run.len - run.n + tok : run.len - 1) : -1;
+      // (rows that are none take row 0 of q: what they make is not written)
       const uint8_t* qp = a.q.p + (ok ? (run.start + tok) * a.q.tok + (head * G + g) * a.q.head : 0);
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (ok) w = *reinterpret_cast<const uint4*>(qp + elem(s) * 2);
-        qf[n][s] = __builtin_bit_cast(bf16x8, w);
+        if constexpr (kQInLds) {
+          if ((n * kSteps + s) % NW == wave) q_lds[n * kSteps + s][lane] = *reinterpret_cast<const uint4*>(qp + elem(s) * 2);
+        } else {
+          qf[n][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + elem(s) * 2));
+        }
       }
     }
+    if constexpr (kQInLds) __syncthreads();
     const int first = a.causal ? run.len - run.n + blk * a.tb : run.len - 1, clear = max(first + 1, 0) / kRowsKeys;
     f32x4 o[NB][DB];
     float m[NB], l[NB];
@@ -671,7 +700,6 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
 #pragma unroll
       for (int i = 0; i < DB; ++i) o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int32_t* table = a.pt.table + seq * a.pt.stride;
     const uint8_t* kbase = a.kp.p + head * a.kp.head;
     const uint8_t* vbase = a.vp.p + head * a.vp.head;
     uint8_t* mine = lds + wave * kRowsKeys * PV;
@@ -680,10 +708,6 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
     uint4 kr[2][kW], vr[kLoads];
     KeyRow kv;             // of key (lane % 32) of the tile whose rows are requested next
     uint32_t have = 0;
-    auto lookup = [&](int t) {
-      const int key = t * kRowsKeys + (lane & 31);
-      return page_entry(a, table, key, run.len);
-    };
     auto request_k = [&]() {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
@@ -708,15 +732,11 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
         vr[j] = *reinterpret_cast<const uint4*>(vbase + row_offset(kv.v, r) + c * 16);
       }
     };
-    const int seen = a.causal ? min(max(run.len - run.n + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
-    const int s0 = t0 * NW + wave, last = min(t1 * NW, (seen + kRowsKeys - 1) / kRowsKeys);   // in tiles of 32 keys
-    int page = -1;
     if (s0 < last) {
-      kv = key_row(a, lookup(s0), s0 * kRowsKeys + (lane & 31), run.len);
+      kv = key_row(a, page0, s0 * kRowsKeys + (lane & 31), run.len);
       have = (uint32_t)__ballot(kv.ok);
       request_k();
       request_v();
-      page = lookup(s0 + NW);
     }
     for (int t = s0; t < last; t += NW) {
       const uint32_t h = have;
@@ -725,10 +745,18 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) s[n][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      int at = lane;
+      if constexpr (kQInLds) asm volatile("" : "+v"(at));   // (read in every turn)
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int i = 0; i < kSteps; ++i) {
+        bf16x8 qs[NB];
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
+        for (int n = 0; n < NB; ++n) {
+          if constexpr (kQInLds) qs[n] = __builtin_bit_cast(bf16x8, q_lds[n * kSteps + i][at]);
+          else qs[n] = qf[n][i];
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
           bf16x8 kf;
           if constexpr (EB == 2) {
             kf = __builtin_bit_cast(bf16x8, kr[kb][i]);
@@ -738,8 +766,9 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
             kf = __builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y));
           }
 #pragma unroll
-          for (int n = 0; n < NB; ++n) s[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][i], s[n][kb], 0, 0, 0);
+          for (int n = 0; n < NB; ++n) s[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qs[n], s[n][kb], 0, 0, 0);
         }
+      }
       // (behind the wave's last keys whatever follows, which nothing uses)
       kv = key_row(a, page, (t + NW) * kRowsKeys + (lane & 31), run.len);
       have = (uint32_t)__ballot(kv.ok);
