@@ -47,16 +47,17 @@ __global__ __launch_bounds__(1024) void paged_attn_join_blocks_kernel(PagedAttnA
 }
 
 // 16 or 32 rows and up to hundreds of parts.  All is latency: one load and a vote find the parts, eight of them are requested at a time.
-// Up to kFewParts of them are joined where the item began, each of the 16 groups with a row of its own; the rows of an item with
-// more are shared by the workgroups whose like worked at it, and the 16 groups share the parts of a row.
+// The rows of an item are shared by the workgroups whose like worked at it.  Where it has up to kFewParts parts each group joins a
+// row of its own, eight groups for the item that began here and eight for the one that goes on or ends here; where it has more,
+// the 16 groups share the parts of a row.
 constexpr int kFewParts = 16;
 __global__ __launch_bounds__(512) void paged_attn_join_rows_kernel(PagedAttnArgs a, int block_rows) {
-  constexpr int kGroups = 16, kAhead = 8, kWords = 512 / kWave;
+  constexpr int kGroups = 16, kHalf = 8, kAhead = 8, kWords = 512 / kWave;
   __shared__ float acc_s[kGroups][128];
   __shared__ float2 ml_s[kGroups];
   __shared__ uint64_t tails[kWords], heads[kWords], lasts[kWords];
   const int me = blockIdx.x, tid = threadIdx.x, grp = tid >> 5, c = (tid & 31) * 4, col = min(c, a.d - 4);
-  const int flags = tid < a.n_wg ? a.desc[tid].x : 0;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), flags = tid < a.n_wg ? a.desc[tid].x : 0;
   const int4 mine = a.desc[me];
   {
     const uint64_t t = __ballot(flags & kPartTail), h = __ballot(flags & kPartHead), l = __ballot(flags & kPartLast);
@@ -75,43 +76,52 @@ __global__ __launch_bounds__(512) void paged_attn_join_rows_kernel(PagedAttnArgs
     while (m == 0 && --i >= 0) m = tails[i];
     return m ? i * 64 + 63 - __clzll((long long)m) : -1;
   };
-  for (int e = 0; e < 2; ++e) {   // what began here, and what lies around this workgroup's part, if any
+  struct Item { int w, parts; int4 desc; };
+  auto item_of = [&](int e) {   // 0: what began here, 1: what lies around this workgroup's part; parts = 0: none
     const int w = e ? begin_of(me) : (mine.x & kPartTail ? me : -1);
-    if (w < 0) continue;
-    const int end = end_of(w), parts = end - w + 1;
-    if (e && (end < me || parts <= kFewParts)) continue;
-    const int4 desc = e ? a.desc[w] : mine;
-    // parts first, first + step, ... of a row
-    auto gather = [&](int row, int first, int step) {
-      Joined j;
-      for (int i0 = first; i0 < parts; i0 += step * kAhead) {
-        float2 ml[kAhead];
-        float4 v[kAhead];
+    const int end = w < 0 ? -1 : end_of(w);
+    if (end < me) return Item{0, 0, mine};
+    return Item{w, end - w + 1, e ? a.desc[w] : mine};
+  };
+  // parts first, first + step, ... of a row
+  auto gather = [&](const Item& it, int row, int first, int step) {
+    Joined j;
+    for (int i0 = first; i0 < it.parts; i0 += step * kAhead) {
+      float2 ml[kAhead];
+      float4 v[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {   // (places in the workspace, whatever they hold)
-          const int i = min(i0 + k * step, parts - 1);
-          const int64_t slot = (2 * (int64_t)(w + i) + (i == 0 ? 1 : 0)) * block_rows + row;
-          ml[k] = a.part_ml[slot];
-          v[k] = *reinterpret_cast<const float4*>(a.part_acc + slot * a.d + col);
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          const int i = i0 + k * step;   // (workgroups inside that had less than a tile to do have no part)
-          if (i < parts && (i == 0 || (heads[(w + i) / 64] >> ((w + i) % 64) & 1))) j.add(ml[k], v[k]);
-        }
+      for (int k = 0; k < kAhead; ++k) {   // (places in the workspace, whatever they hold)
+        const int i = min(i0 + k * step, it.parts - 1);
+        const int64_t slot = (2 * (int64_t)(it.w + i) + (i == 0 ? 1 : 0)) * block_rows + row;
+        ml[k] = a.part_ml[slot];
+        v[k] = *reinterpret_cast<const float4*>(a.part_acc + slot * a.d + col);
       }
-      return j;
-    };
-    auto finish = [&](const Joined& j, int row) {
-      const int tl = row / a.G;
-      if (c < a.d) j.finish(a, (int64_t)desc.y + tl, desc.z * a.G + row - tl * a.G, c);
-    };
-    if (parts <= kFewParts) {
-      for (int row = grp; row < desc.w; row += kGroups) finish(gather(row, 0, 1), row);
-      continue;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = i0 + k * step;   // (workgroups inside that had less than a tile to do have no part)
+        if (i < it.parts && (i == 0 || (heads[(it.w + i) / 64] >> ((it.w + i) % 64) & 1))) j.add(ml[k], v[k]);
+      }
     }
-    for (int row = me - w; row < desc.w; row += parts) {
-      const Joined j = gather(row, grp, kGroups);
+    return j;
+  };
+  auto finish = [&](const Item& it, const Joined& j, int row) {
+    const int tl = row / a.G;
+    if (c < a.d) j.finish(a, (int64_t)it.desc.y + tl, it.desc.z * a.G + row - tl * a.G, c);
+  };
+  const Item own = item_of(0), around = item_of(1);
+  auto join_few = [&](const Item& it, bool is_own) {
+    if (it.parts == 0 || it.parts > kFewParts) return;
+    const bool alone = it.desc.w <= kHalf;   // (joined where it began, whose descriptor is at hand)
+    if (alone && !is_own) return;
+    const int g = grp % kHalf;
+    for (int row = alone ? g : me - it.w + g * it.parts; row < it.desc.w; row += alone ? kHalf : kHalf * it.parts) finish(it, gather(it, row, 0, 1), row);
+  };
+  if (wave < kWords / 2) join_few(own, true);
+  else join_few(around, false);
+  auto join_many = [&](const Item& it) {
+    if (it.parts <= kFewParts) return;
+    for (int row = me - it.w; row < it.desc.w; row += it.parts) {
+      const Joined j = gather(it, row, grp, kGroups);
       __syncthreads();   // (the row before)
       if (c < a.d) *reinterpret_cast<float4*>(&acc_s[grp][c]) = make_float4(j.x[0], j.x[1], j.x[2], j.x[3]);
       if (c == 0) ml_s[grp] = make_float2(j.m, j.l);
@@ -120,10 +130,12 @@ __global__ __launch_bounds__(512) void paged_attn_join_rows_kernel(PagedAttnArgs
         Joined all;
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) all.add(ml_s[i], *reinterpret_cast<const float4*>(&acc_s[i][col]));
-        finish(all, row);
+        finish(it, all, row);
       }
     }
-  }
+  };
+  join_many(own);
+  join_many(around);
 }
 
 int paged_attn_block_rows(int G, long rows) { return G <= 16 && rows <= 16 ? 16 : G <= 32 && rows <= 32 ? 32 : kTileRows; }

@@ -652,8 +652,9 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
   constexpr int PV = RowsPitch<D>::v;
   constexpr int kVBytes = NW * kRowsKeys * PV, kMergeBytes = NW * BR * (D * 4 + 8);
   __shared__ __attribute__((aligned(16))) uint8_t lds[kVBytes > kMergeBytes ? kVBytes : kMergeBytes];
-  // Q of two row blocks waits in LDS, in operand order: with it in registers heads of 128 spilled 54 of theirs
-  constexpr bool kQInLds = NB == 2;
+  // Q of two row blocks of long heads waits in LDS, in operand order: in registers, heads of 128 spilled 54 of theirs (259 us
+  // against 234, 16 sequences of 16K keys, 8 tokens each, 32 heads on 8), while heads of 64 have room for it (41.4 us against 42.4)
+  constexpr bool kQInLds = NB == 2 && D > 64;
   __shared__ uint4 q_lds[kQInLds ? NB * kSteps : 1][kWave];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, col = lane & 15, quarter = lane >> 4;
 
