@@ -62,6 +62,16 @@ __device__ __forceinline__ uint32_t e5m2x2_to_bf16x2(uint32_t w) {
   return (__float_as_uint(f[0]) >> 16) | (__float_as_uint(f[1]) & 0xffff0000u);
 }
 
+// two fp32 as two bf16, nearest even, and four as four E5M2 (v_cvt_pk_bf8_f32: f32_to_e5m2's result for every fp32 pattern)
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+  const f32x2_t x = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf2));
+}
+__device__ __forceinline__ uint32_t pack_e5m2(float a, float b, float c, float d) {
+  return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(c, d, __builtin_amdgcn_cvt_pk_bf8_f32(a, b, 0, false), true);
+}
+
 // fp64 -> E5M2 with a single rounding (nearest, ties to even; beyond the largest finite value 57344
 // the result is infinity, as in IEEE 754): fp64 -> fp32 by round-to-odd, then
 // the fp32 is rounded at its 21st fraction bit, in integer arithmetic so that a carry moves into the

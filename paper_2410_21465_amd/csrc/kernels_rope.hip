@@ -26,11 +26,9 @@ struct Piece {
 template <int P, int EB>
 __device__ __forceinline__ void pack_f32(const float (&x)[P], Piece<P, EB>& o) {
 #pragma unroll
-  for (int i = 0; i < RawWords<P, EB>::n; ++i) o.w[i] = 0u;
-#pragma unroll
-  for (int e = 0; e < P; ++e) {
-    if constexpr (EB == 2) o.w[e / 2] |= (uint32_t)f32_to_bf16(x[e]) << (16 * (e & 1));
-    else o.w[e / 4] |= (uint32_t)f32_to_e5m2(x[e]) << (8 * (e & 3));
+  for (int i = 0; i < RawWords<P, EB>::n; ++i) {
+    if constexpr (EB == 2) o.w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+    else o.w[i] = pack_e5m2(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
   }
 }
 

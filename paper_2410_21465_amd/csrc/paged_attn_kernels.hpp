@@ -253,12 +253,6 @@ __device__ __forceinline__ void for_items(const PagedAttnArgs& a, F&& work) {
 }
 
 // ---- elements -------------------------------------------------------------------------------------------------------
-// two fp32 as two bf16, nearest even
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  typedef float f2 __attribute__((ext_vector_type(2)));
-  const f2 x = {lo, hi};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-}
 // upper halves of two 32-bit words
 __device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
 // four E5M2 bytes as four bf16 (exact)
