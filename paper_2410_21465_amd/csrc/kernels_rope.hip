@@ -55,6 +55,34 @@ __device__ __forceinline__ void slot_at(const RopeArgs& r, int slot, bool turned
   b = apart ? a + r.rot / 2 : a + P;
 }
 
+// The two pieces of a slot, as one access of 16 bytes where they lie side by side and are of 8 (rotate's FP8 heads, turned by pairs
+// side by side or not turned: 104 us -> 85 us for 20K tokens of three sequences, 32 heads of 96).
+typedef uint32_t U32x4 __attribute__((ext_vector_type(4), aligned(8)));
+template <int P, int EB>
+__device__ __forceinline__ void load_pieces(const uint8_t* p, int a, int b, Piece<P, EB>& x, Piece<P, EB>& y) {
+  if constexpr (P * EB == 8) {
+    if (b == a + P) {
+      const U32x4 v = *reinterpret_cast<const U32x4*>(p + a * EB);
+      x.w[0] = v[0]; x.w[1] = v[1]; y.w[0] = v[2]; y.w[1] = v[3];
+      return;
+    }
+  }
+  load_raw<P, EB>(p + a * EB, x.w);
+  load_raw<P, EB>(p + b * EB, y.w);
+}
+template <int P, int EB>
+__device__ __forceinline__ void store_pieces(uint8_t* p, int a, int b, const Piece<P, EB>& x, const Piece<P, EB>& y) {
+  if constexpr (P * EB == 8) {
+    if (b == a + P) {
+      const U32x4 v = {x.w[0], x.w[1], y.w[0], y.w[1]};
+      *reinterpret_cast<U32x4*>(p + a * EB) = v;
+      return;
+    }
+  }
+  store_raw<P, EB>(p + a * EB, x.w);
+  store_raw<P, EB>(p + b * EB, y.w);
+}
+
 // One slot of n <= kHeadsPerBlock heads, src and dst at the first head.
 template <int P, int EBI, int EBO>
 __device__ __forceinline__ void turn_heads(const uint8_t* src, int64_t src_head, uint8_t* dst, int64_t dst_head, int n, int a, int b,
@@ -62,10 +90,7 @@ __device__ __forceinline__ void turn_heads(const uint8_t* src, int64_t src_head,
   Piece<P, EBI> x[kHeadsPerBlock], y[kHeadsPerBlock];
 #pragma unroll
   for (int h = 0; h < kHeadsPerBlock; ++h)
-    if (h < n) {
-      load_raw<P, EBI>(src + h * src_head + a * EBI, x[h].w);
-      load_raw<P, EBI>(src + h * src_head + b * EBI, y[h].w);
-    }
+    if (h < n) load_pieces<P, EBI>(src + h * src_head, a, b, x[h], y[h]);
 #pragma unroll
   for (int h = 0; h < kHeadsPerBlock; ++h) {
     if (h >= n) break;
@@ -98,8 +123,7 @@ __device__ __forceinline__ void turn_heads(const uint8_t* src, int64_t src_head,
       pack_f32<P, EBO>(p, ox);
       pack_f32<P, EBO>(q, oy);
     }
-    store_raw<P, EBO>(dst + h * dst_head + a * EBO, ox.w);
-    store_raw<P, EBO>(dst + h * dst_head + b * EBO, oy.w);
+    store_pieces<P, EBO>(dst + h * dst_head, a, b, ox, oy);
   }
 }
 
