@@ -86,7 +86,8 @@ int rope_table(const shadowkv_rope* r, double* w) {   // radians per position
   return n;
 }
 
-int check_rope(const shadowkv_rope* r) {
+// w: the frequencies, unless the caller's own replace them
+int check_rope(const shadowkv_rope* r, double (&w)[kMaxHalfDim]) {
   if (!r) return fail_inval("rope is NULL");
   if (!known_head_dim(r->head_dim)) return fail_inval("head_dim must be 64, 96 or 128");
   const int rot = r->rot_dim ? r->rot_dim : r->head_dim;
@@ -107,14 +108,13 @@ int check_rope(const shadowkv_rope* r) {
     if (!std::isfinite(r->low) || !std::isfinite(r->high) || !(r->low < r->high)) return fail_inval("low and high must be finite, low < high");
   }
   if (r->scaling == SHADOWKV_ROPE_YARN && (!(r->low > 0.0) || !(r->theta > 1.0))) return fail_inval("YARN needs low > 0 and theta > 1");
-  double w[kMaxHalfDim];
   const int n = rope_table(r, w);
   for (int i = 0; i < n; ++i)
     if (!std::isfinite(w[i])) return fail_inval("the frequencies are not finite");
   return SHADOWKV_OK;
 }
 
-RopeArgs rope_args(const shadowkv_rope* r, bool transposed) {
+RopeArgs rope_args(const shadowkv_rope* r, const double (&w)[kMaxHalfDim], bool transposed) {
   RopeArgs a{};
   a.d = r->head_dim;
   a.rot = r->rot_dim ? r->rot_dim : r->head_dim;
@@ -123,10 +123,8 @@ RopeArgs rope_args(const shadowkv_rope* r, bool transposed) {
   a.mag = (float)(r->magnitude != 0.0 ? r->magnitude : by_itself);
   a.sign = transposed ? -1.f : 1.f;
   a.inv_freq = r->inv_freq;
-  if (!r->inv_freq) {
-    const int n = rope_table(r, a.rev);
-    for (int i = 0; i < n; ++i) a.rev[i] /= 6.283185307179586476925;
-  }
+  if (!r->inv_freq)
+    for (int i = 0; i < a.rot / 2; ++i) a.rev[i] = w[i] / 6.283185307179586476925;
   return a;
 }
 
@@ -198,17 +196,19 @@ int paged_attn_layout(const shadowkv_paged_cache* c, int hq, int n_tokens, Paged
 extern "C" {
 
 int shadowkv_rope_frequencies(const shadowkv_rope* rope, double* out) {
-  const int rc = check_rope(rope);
+  double w[kMaxHalfDim];
+  const int rc = check_rope(rope, w);
   if (rc != SHADOWKV_OK) return rc;
   if (!out) return fail_inval("out is NULL");
   if (rope->inv_freq) return fail_inval("the frequencies are in inv_freq, on the device");
-  rope_table(rope, out);
+  std::copy_n(w, (rope->rot_dim ? rope->rot_dim : rope->head_dim) / 2, out);
   return SHADOWKV_OK;
 }
 
 int shadowkv_rotate(const shadowkv_rope* rope, const shadowkv_heads* x, const shadowkv_heads* out, const int32_t* positions,
                     const int32_t* pos_offset, int32_t transposed, void* stream) {
-  int rc = check_rope(rope);
+  double w[kMaxHalfDim];
+  int rc = check_rope(rope, w);
   if (rc == SHADOWKV_OK) rc = check_heads("x", x, rope->head_dim, false);
   if (rc == SHADOWKV_OK) rc = check_heads("out", out, rope->head_dim, true);
   if (rc != SHADOWKV_OK) return rc;
@@ -220,7 +220,7 @@ int shadowkv_rotate(const shadowkv_rope* rope, const shadowkv_heads* x, const sh
     if (a < b + extent_bytes(out, rope->head_dim) && b < a + extent_bytes(x, rope->head_dim) && x->data == out->data)
       return fail_inval("out begins where x does and is laid out differently");
   }
-  const hipError_t e = launch_rotate(rope_args(rope, transposed != 0), heads_arg(x), heads_arg(out), positions, pos_offset, x->n_seqs, x->n_tokens,
+  const hipError_t e = launch_rotate(rope_args(rope, w, transposed != 0), heads_arg(x), heads_arg(out), positions, pos_offset, x->n_seqs, x->n_tokens,
                                      x->n_heads, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SHADOWKV_OK : fail_hip("rotate", e);
 }
@@ -231,8 +231,9 @@ int shadowkv_paged_append(const shadowkv_paged_cache* cache, const shadowkv_rope
   int rc = check_cache(cache, true, true);
   if (rc != SHADOWKV_OK) return rc;
   const int d = cache->head_dim;
+  double w[kMaxHalfDim];
   if (rope) {
-    rc = check_rope(rope);
+    rc = check_rope(rope, w);
     if (rc != SHADOWKV_OK) return rc;
     if (rope->head_dim != d) return fail_inval("rope and cache differ in head_dim");
   }
@@ -254,7 +255,7 @@ int shadowkv_paged_append(const shadowkv_paged_cache* cache, const shadowkv_rope
   if (k->n_tokens == 0) return SHADOWKV_OK;
   const int eb = elem_bytes(cache->kv_dtype);
   RopeArgs ra{};
-  if (rope) ra = rope_args(rope, false);
+  if (rope) ra = rope_args(rope, w, false);
   const hipError_t e = launch_paged_append(
       rope ? &ra : nullptr, pages_arg(cache->k, cache->k_page_stride, cache->k_head_stride, cache->k_token_stride, eb),
       pages_arg(cache->v, cache->v_page_stride, cache->v_head_stride, cache->v_token_stride, eb), table_arg(cache), eb, heads_arg(k), heads_arg(v),
