@@ -25,34 +25,15 @@ struct Joined {   // a row's state as parts are added
   }
 };
 
-// 128 rows, two or three parts: workgroup w joins the item that its like began, a row per group at a time.
-__global__ __launch_bounds__(1024) void paged_attn_join_blocks_kernel(PagedAttnArgs a, int block_rows) {
-  const int w = blockIdx.x, c = ((int)threadIdx.x & 31) * 4;
-  const int4 desc = a.desc[w];
-  if (!(desc.x & kPartTail) || c >= a.d) return;
-  for (int row = threadIdx.x >> 5; row < desc.w; row += 32) {
-    const int tl = row / a.G, g = row - tl * a.G;
-    Joined j;
-    auto part = [&](int64_t slot) {
-      j.add(a.part_ml[slot * block_rows + row], *reinterpret_cast<const float4*>(a.part_acc + (slot * block_rows + row) * a.d + c));
-    };
-    part(2 * (int64_t)w + 1);
-    for (int i = w + 1; i < a.n_wg; ++i) {
-      const int f = a.desc[i].x;
-      if (f & kPartHead) part(2 * (int64_t)i);
-      if (f & kPartLast) break;
-    }
-    j.finish(a, (int64_t)desc.y + tl, desc.z * a.G + g, c);
-  }
-}
-
-// 16 or 32 rows and up to hundreds of parts.  All is latency: one load and a vote find the parts, eight of them are requested at a time.
+// All is latency: one load and a vote find the parts, eight of them are requested at a time.
 // The rows of an item are shared by the workgroups whose like worked at it.  Where it has up to kFewParts parts each group joins a
-// row of its own, eight groups for the item that began here and eight for the one that goes on or ends here; where it has more,
-// the 16 groups share the parts of a row.
+// row of its own, half of the groups for the item that began here and half for the one that goes on or ends here; where it has
+// more, the groups share the parts of a row.
 constexpr int kFewParts = 16;
-__global__ __launch_bounds__(512) void paged_attn_join_rows_kernel(PagedAttnArgs a, int block_rows) {
-  constexpr int kGroups = 16, kHalf = 8, kAhead = 8, kWords = 512 / kWave;
+template <int NT>
+__global__ __launch_bounds__(NT) void paged_attn_join_kernel(PagedAttnArgs a, int block_rows) {
+  static_assert(NT >= 512);   // (a thread per workgroup of the first kernel)
+  constexpr int kGroups = NT / 32, kHalf = kGroups / 2, kAhead = 8, kWords = NT / kWave;
   __shared__ float acc_s[kGroups][128];
   __shared__ float2 ml_s[kGroups];
   __shared__ uint64_t tails[kWords], heads[kWords], lasts[kWords];
@@ -83,26 +64,25 @@ __global__ __launch_bounds__(512) void paged_attn_join_rows_kernel(PagedAttnArgs
     if (end < me) return Item{0, 0, mine};
     return Item{w, end - w + 1, e ? a.desc[w] : mine};
   };
-  // parts first, first + step, ... of a row
-  auto gather = [&](const Item& it, int row, int first, int step) {
-    Joined j;
-    for (int i0 = first; i0 < it.parts; i0 += step * kAhead) {
+  // parts first, first + step, ... of R rows that lie row_step apart, kAhead / R parts at a time
+  auto gather = [&](auto rows, const Item& it, int row, int row_step, int first, int step, Joined (&j)[decltype(rows)::value]) {
+    constexpr int R = decltype(rows)::value, kParts = kAhead / R;
+    for (int i0 = first; i0 < it.parts; i0 += step * kParts) {
       float2 ml[kAhead];
       float4 v[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {   // (places in the workspace, whatever they hold)
-        const int i = min(i0 + k * step, it.parts - 1);
-        const int64_t slot = (2 * (int64_t)(it.w + i) + (i == 0 ? 1 : 0)) * block_rows + row;
+        const int i = min(i0 + k % kParts * step, it.parts - 1);
+        const int64_t slot = (2 * (int64_t)(it.w + i) + (i == 0 ? 1 : 0)) * block_rows + min(row + k / kParts * row_step, it.desc.w - 1);
         ml[k] = a.part_ml[slot];
         v[k] = *reinterpret_cast<const float4*>(a.part_acc + slot * a.d + col);
       }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const int i = i0 + k * step;   // (workgroups inside that had less than a tile to do have no part)
-        if (i < it.parts && (i == 0 || (heads[(it.w + i) / 64] >> ((it.w + i) % 64) & 1))) j.add(ml[k], v[k]);
+        const int i = i0 + k % kParts * step;   // (workgroups inside that had less than a tile to do have no part)
+        if (i < it.parts && (i == 0 || (heads[(it.w + i) / 64] >> ((it.w + i) % 64) & 1))) j[k / kParts].add(ml[k], v[k]);
       }
     }
-    return j;
   };
   auto finish = [&](const Item& it, const Joined& j, int row) {
     const int tl = row / a.G;
@@ -113,15 +93,29 @@ __global__ __launch_bounds__(512) void paged_attn_join_rows_kernel(PagedAttnArgs
     if (it.parts == 0 || it.parts > kFewParts) return;
     const bool alone = it.desc.w <= kHalf;   // (joined where it began, whose descriptor is at hand)
     if (alone && !is_own) return;
-    const int g = grp % kHalf;
-    for (int row = alone ? g : me - it.w + g * it.parts; row < it.desc.w; row += alone ? kHalf : kHalf * it.parts) finish(it, gather(it, row, 0, 1), row);
+    const int first = alone ? grp % kHalf : me - it.w + grp % kHalf * it.parts, step = alone ? kHalf : kHalf * it.parts;
+    auto go = [&](auto rows) {
+      constexpr int R = decltype(rows)::value;
+      for (int row = first; row < it.desc.w; row += R * step) {
+        Joined j[R];
+        gather(rows, it, row, step, 0, 1, j);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          if (row + r * step < it.desc.w) finish(it, j[r], row + r * step);
+      }
+    };
+    if (it.parts <= 2) go(std::integral_constant<int, 4>{});
+    else if (it.parts <= 4) go(std::integral_constant<int, 2>{});
+    else go(std::integral_constant<int, 1>{});
   };
   if (wave < kWords / 2) join_few(own, true);
   else join_few(around, false);
   auto join_many = [&](const Item& it) {
     if (it.parts <= kFewParts) return;
     for (int row = me - it.w; row < it.desc.w; row += it.parts) {
-      const Joined j = gather(it, row, grp, kGroups);
+      Joined js[1];
+      gather(std::integral_constant<int, 1>{}, it, row, 0, grp, kGroups, js);
+      const Joined& j = js[0];
       __syncthreads();   // (the row before)
       if (c < a.d) *reinterpret_cast<float4*>(&acc_s[grp][c]) = make_float4(j.x[0], j.x[1], j.x[2], j.x[3]);
       if (c == 0) ml_s[grp] = make_float2(j.m, j.l);
@@ -144,8 +138,8 @@ int paged_attn_workgroups(int block_rows) { return 512; }   // two per compute u
 hipError_t launch_paged_attention(PagedAttnArgs a, int block_rows, hipStream_t st) {
   hipError_t e = a.kv_bytes == 1 ? launch_paged_attn_fp8(a, block_rows, st) : launch_paged_attn_eb<2>(a, block_rows, st);
   if (e != hipSuccess) return e;
-  if (block_rows == kTileRows) hipLaunchKernelGGL(paged_attn_join_blocks_kernel, dim3(a.n_wg), dim3(1024), 0, st, a, block_rows);
-  else hipLaunchKernelGGL(paged_attn_join_rows_kernel, dim3(a.n_wg), dim3(512), 0, st, a, block_rows);
+  if (block_rows == kTileRows) hipLaunchKernelGGL(paged_attn_join_kernel<1024>, dim3(a.n_wg), dim3(1024), 0, st, a, block_rows);
+  else hipLaunchKernelGGL(paged_attn_join_kernel<512>, dim3(a.n_wg), dim3(512), 0, st, a, block_rows);
   return hipGetLastError();
 }
 
