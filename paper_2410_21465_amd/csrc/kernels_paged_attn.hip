@@ -26,7 +26,7 @@ struct Joined {   // a row's state as parts are added
 };
 
 // All is latency: one load and a vote find the parts, eight of them are requested at a time.
-// The rows of an item are shared by the workgroups whose like worked at it.  Where it has up to kFewParts parts each group joins a
+// The rows of an item are shared by the workgroups whose like worked at it.  Where it has few parts each group joins a
 // row of its own, half of the groups for the item that began here and half for the one that goes on or ends here; where it has
 // more, the groups share the parts of a row.
 constexpr int kFewParts = 16;
@@ -89,8 +89,10 @@ __global__ __launch_bounds__(NT) void paged_attn_join_kernel(PagedAttnArgs a, in
     if (c < a.d) j.finish(a, (int64_t)it.desc.y + tl, it.desc.z * a.G + row - tl * a.G, c);
   };
   const Item own = item_of(0), around = item_of(1);
+  // (one way takes a trip to memory per eight parts, the other one per row of a workgroup, of which it has rows / parts)
+  auto few = [&](const Item& it) { return it.parts <= kFewParts || it.parts * it.parts <= 12 * it.desc.w; };
   auto join_few = [&](const Item& it, bool is_own) {
-    if (it.parts == 0 || it.parts > kFewParts) return;
+    if (it.parts == 0 || !few(it)) return;
     const bool alone = it.desc.w <= kHalf;   // (joined where it began, whose descriptor is at hand)
     if (alone && !is_own) return;
     const int first = alone ? grp % kHalf : me - it.w + grp % kHalf * it.parts, step = alone ? kHalf : kHalf * it.parts;
@@ -111,7 +113,7 @@ __global__ __launch_bounds__(NT) void paged_attn_join_kernel(PagedAttnArgs a, in
   if (wave < kWords / 2) join_few(own, true);
   else join_few(around, false);
   auto join_many = [&](const Item& it) {
-    if (it.parts <= kFewParts) return;
+    if (few(it)) return;
     for (int row = me - it.w; row < it.desc.w; row += it.parts) {
       Joined js[1];
       gather(std::integral_constant<int, 1>{}, it, row, 0, grp, kGroups, js);
