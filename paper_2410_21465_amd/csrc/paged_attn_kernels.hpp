@@ -126,7 +126,8 @@ __device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* foun
   const int64_t each = quotient(total, n);
   const int more = (int)(total - each * n);   // (below n, and n below 2^11)
   const int64_t cut0 = each * w + more * w / n, cut1 = each * (w + 1) + more * (w + 1) / n;
-  // A cut within `near` keys of an item's end is made there: a split item costs its parts' way through memory.
+  // A cut within `near` keys of an item's end is made there: a split item costs its parts' way through memory (a prompt of 8K tokens,
+  // together with the order of the blocks: 686 -> 620 us).
   const int64_t near = min(max((int64_t)kItemKeys, each / 32), each / 8);
   int64_t before = 0;   // work of the sequences before these 64
   if (lane == 0) found[4] = w + 1 == n ? total : -1;
@@ -316,8 +317,14 @@ __device__ __forceinline__ uint64_t row_offset(uint32_t units, int src) {   // b
 
 // ---- 128 rows: the four waves of a workgroup take 32 rows each -----------------------------------------------------------
 // Tiles of 64 keys, K and V through registers into two LDS buffers: while one tile is multiplied the next is on its way, one barrier a
-// tile.  FP8 is widened to bf16 between registers and LDS.  Per tile a wave issues 2 x D / 8 v_mfma_f32_32x32x16_bf16.
+// tile.  FP8 is widened to bf16 between registers and LDS.  Per tile a wave issues D / 4 v_mfma_f32_32x32x16_bf16.
 // Row pitches: K's 16-byte reads of 16 rows and V's transposing reads of four rows of 64 bytes fall on all 64 banks.
+//
+// Bound by the matrix pipe and the softmax's vector instructions, each busy for 44 % of a prompt's cycles: with two waves per SIMD
+// (256 registers a wave) they overlap only in part.  32/8 heads of 128: a prompt of 8K tokens 605 us = 0.91 PFLOP/s, 2K tokens after
+// 28K 1.04 ms = 0.94 PFLOP/s (a bf16 product of 8192^3 reaches 1.3; zeros in place of random data run a third faster there and a
+// quarter here: both are held by power).  Slower: the next tile's first half multiplied behind the weights (710 against 687 us),
+// 64 rows a wave and one wave per SIMD (0.5 to 0.7 of the rate), the maximum settled per 32 keys (643 against 621 us).
 constexpr int kTileKeys = 64, kTileRows = 128, kTileNT = 256;
 template <int D>
 struct TilePitch {
@@ -452,7 +459,7 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
       uint8_t* buf = lds + ((t - t0) & 1) * TilePitch<D>::bytes;
       uint8_t* next = lds + (((t - t0) & 1) ^ 1) * TilePitch<D>::bytes;
       // The next tile, or behind the last one (t + 1 == t1) whatever follows, which nothing uses: no branch, so that the loads stay
-      // in flight (where a branch joined them, the compiler's copies waited for them at once: 715 TFLOP/s against %NEW%).
+      // in flight (where a branch joined them, the compiler's copies waited for them at once).
       kv = key_row(a, page_next, (t + 1) * kTileKeys + lane, run.len);
       page_next = page_entry(a, table, (t + 2) * kTileKeys + lane, run.len);
       have = __ballot(kv.ok);
@@ -472,7 +479,7 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
           for (int e = 0; e < 4; ++e) f[e] = *reinterpret_cast<const uint4*>(kp + (e & 1) * 32 * PK + (i + (e >> 1)) * 32);
         };
         read(0, kf[0]);
-        __builtin_amdgcn_s_setprio(1);   // over the other workgroup's wave, which forms weights meanwhile
+        __builtin_amdgcn_s_setprio(1);   // over the other workgroup's wave, which forms weights meanwhile (a prompt of 8K: 620 -> 607 us)
 #pragma unroll
         for (int i = 0; i < QS; i += 2) {
           if (i + 2 < QS) read(i + 2, kf[(i / 2 + 1) % 2]);
@@ -484,7 +491,8 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
         }
       }
       __builtin_amdgcn_s_setprio(0);
-      // (FP8's conversions go behind the first weights: 343 us that way, 347 before)
+      // (FP8's conversions go behind the first weights: 341 us against 347 in four ragged chunks of up to 1.3K tokens; bf16, which has
+      // nothing to convert, the other way round: 1052 us against 1064 in 2K tokens after 28K)
       if constexpr (EB == 2) {
         store(next, PK);
         request(vbase, at_v);
@@ -631,7 +639,12 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
 // holds eight elements of one key, which four lanes of a row request as 64 neighbouring bytes; the order of the elements inside
 // the product is free as long as Q's is the same.  V goes through a piece of LDS of the wave's own, so nothing waits for
 // another wave before the end.  The next 32 keys are requested as soon as the registers are free.  The softmax weights enter as two bf16 terms:
-// the matrix pipe has the time (a wave's 32 keys take it 0.4 us x 1/2.4 of memory's).
+// the matrix pipe has the time (32 keys of two waves take a SIMD's 0.3 us, and their bytes 6 us at 5.2 TB/s).
+// 16 sequences of 32K keys, a token each, 32/8 heads of 128: 243 us + 6 for the join, 5.5 TB/s (a large copy: 5.0 to 5.4, read and
+// written); one of 1M keys, 32/2 heads: 195 us + 14; one of 4K keys: 15 us + 6, a chain of latencies (the share 3, page table and Q 2, keys 3,
+// the merge 2 us).  For 17 to 32 rows the kernel for 128 would take 49 us against 39 (24 chats' drafts, FP8, 14/2 heads of 64), 180
+// against 119 (16 sequences of 16K FP8 keys, 8 tokens each, 32/8 heads of 128), 398 against 351 (bf16, heads of 96, 20 rows), but 219
+// against 226 and 34 against 40 with bf16 heads of 128, whose registers do not hold two blocks of rows: the price of the second term there.
 constexpr int kRowsKeys = 32, kRowsNT = 256;
 template <int D>
 struct RowsPitch {
