@@ -369,7 +369,7 @@ int shadowkv_rope_frequencies(const shadowkv_rope *rope, double *out);
  *   out        same sizes, bf16 or E5M2, any strides; may be x itself (same pointer, type and strides)
  *   positions  dev [n_seqs, n_tokens] int32 or NULL: position of every token
  *   pos_offset dev [n_seqs] int32 or NULL (only with positions == NULL): token t of sequence i is at pos_offset[i] + t
- * pre-RoPE keys [b, s, h_kv*d] turned into [b, h_kv, s, d] is one call with those strides.
+ * pre-RoPE keys [b, s, h_kv*d] turned into [b, h_kv, s, d] is one call with those strides.  At most 2^27 tokens a call.
  */
 int shadowkv_rotate(const shadowkv_rope *rope, const shadowkv_heads *x, const shadowkv_heads *out,
                     const int32_t *positions, const int32_t *pos_offset, int32_t transposed, void *stream);
@@ -409,7 +409,7 @@ typedef struct shadowkv_paged_cache {
  *   seq_starts dev [batch + 1] int32, ascending; NULL: T / batch tokens of every sequence (batch must divide T)
  *   kv_lens    dev [batch] int32
  *   pos_offset dev [batch] int32 or NULL (0)
- * No place may be written twice in a call.
+ * No place may be written twice in a call.  T <= 2^27.
  */
 int shadowkv_paged_append(const shadowkv_paged_cache *cache, const shadowkv_rope *rope, const shadowkv_heads *k,
                           const shadowkv_heads *v, const shadowkv_heads *q, const shadowkv_heads *q_out,

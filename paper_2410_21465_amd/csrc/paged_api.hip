@@ -10,6 +10,9 @@ using namespace skv;
 
 namespace {
 
+constexpr double kLog2e = 1.4426950408889634074;
+constexpr int64_t kMaxLaunchTokens = (int64_t)1 << 27;   // of a launch with up to 16 threads a token: 2^31 threads
+
 int elem_bytes(int dtype) { return dtype == SHADOWKV_KV_FP8_E5M2 ? 1 : 2; }
 bool known_dtype(int dtype) { return dtype == SHADOWKV_KV_BF16 || dtype == SHADOWKV_KV_FP8_E5M2; }
 bool known_head_dim(int d) { return d == 64 || d == 96 || d == 128; }
@@ -21,7 +24,7 @@ int check_strides(const char* name, const int64_t* stride, const int64_t* size, 
   int k = 0;
   for (int i = 0; i < n; ++i) {
     if (size[i] <= 1) continue;
-    if (stride[i] < 0 || stride[i] * eb % 16 || stride[i] > ((int64_t)1 << 48))
+    if (stride[i] < 0 || stride[i] > ((int64_t)1 << 48) || stride[i] * eb % 16)
       return fail_inval("%s: strides must be multiples of 16 bytes and not negative", name);
     st[k] = stride[i]; sz[k] = size[i]; ++k;
   }
@@ -96,7 +99,7 @@ int check_rope(const shadowkv_rope* r, double (&w)[kMaxHalfDim]) {
     return fail_inval("layout must be SHADOWKV_ROPE_HALF or SHADOWKV_ROPE_INTERLEAVED");
   if (r->scaling < SHADOWKV_ROPE_PLAIN || r->scaling > SHADOWKV_ROPE_YARN) return fail_inval("unknown frequency scaling");
   if (r->reserved) return fail_inval("reserved must be 0");
-  if (!std::isfinite(r->magnitude) || r->magnitude < 0.0) return fail_inval("magnitude must be finite and >= 0");
+  if (!std::isfinite((float)r->magnitude) || r->magnitude < 0.0) return fail_inval("magnitude must be finite (in fp32) and >= 0");
   if (r->inv_freq) {
     if (r->scaling != SHADOWKV_ROPE_PLAIN) return fail_inval("inv_freq replaces the frequencies: scaling must be SHADOWKV_ROPE_PLAIN");
     return SHADOWKV_OK;
@@ -214,6 +217,7 @@ int shadowkv_rotate(const shadowkv_rope* rope, const shadowkv_heads* x, const sh
   if (rc != SHADOWKV_OK) return rc;
   if (x->n_seqs != out->n_seqs || x->n_tokens != out->n_tokens || x->n_heads != out->n_heads) return fail_inval("x and out differ in size");
   if (positions && pos_offset) return fail_inval("positions and pos_offset exclude each other");
+  if ((int64_t)x->n_seqs * x->n_tokens > kMaxLaunchTokens) return fail_inval("more than 2^27 tokens");
   if (x->n_seqs == 0 || x->n_tokens == 0) return SHADOWKV_OK;
   if (!same_array(x, out)) {
     const char *a = static_cast<const char*>(x->data), *b = static_cast<const char*>(out->data);
@@ -252,6 +256,7 @@ int shadowkv_paged_append(const shadowkv_paged_cache* cache, const shadowkv_rope
   if (q && (q->dtype != SHADOWKV_KV_BF16 || q_out->dtype != SHADOWKV_KV_BF16)) return fail_inval("q and q_out must be bf16");
   rc = check_runs(cache, k, seq_starts, kv_lens);
   if (rc != SHADOWKV_OK) return rc;
+  if (k->n_tokens > kMaxLaunchTokens) return fail_inval("more than 2^27 tokens");
   if (k->n_tokens == 0) return SHADOWKV_OK;
   const int eb = elem_bytes(cache->kv_dtype);
   RopeArgs ra{};
@@ -282,7 +287,7 @@ int shadowkv_paged_attention(const shadowkv_paged_cache* cache, const shadowkv_h
   if (q->n_seqs != 1 || out->n_seqs != 1) return fail_inval("q and out are one run of tokens: n_seqs must be 1");
   if (q->n_tokens != out->n_tokens || q->n_heads != out->n_heads) return fail_inval("q and out differ in size");
   if (q->dtype != SHADOWKV_KV_BF16 || out->dtype != SHADOWKV_KV_BF16) return fail_inval("q and out must be bf16");
-  if (!(softmax_scale >= 0.0) || !std::isfinite(softmax_scale)) return fail_inval("softmax_scale must be finite and >= 0");
+  if (!(softmax_scale >= 0.0) || !std::isfinite((float)(softmax_scale * kLog2e))) return fail_inval("softmax_scale must be finite (in fp32) and >= 0");
   rc = check_runs(cache, q, seq_starts, kv_lens);
   if (rc != SHADOWKV_OK) return rc;
   PagedAttnLayout L;
@@ -301,7 +306,7 @@ int shadowkv_paged_attention(const shadowkv_paged_cache* cache, const shadowkv_h
   a.pt = table_arg(cache);
   a.runs = RunsArg{seq_starts, kv_lens, cache->batch, q->n_tokens};
   a.hq = q->n_heads; a.hkv = cache->n_kv_heads; a.G = L.G; a.d = d; a.kv_bytes = eb; a.causal = causal != 0;
-  a.scale_log2 = (float)((softmax_scale != 0.0 ? softmax_scale : 1.0 / std::sqrt((double)d)) * 1.4426950408889634074);
+  a.scale_log2 = (float)((softmax_scale != 0.0 ? softmax_scale : 1.0 / std::sqrt((double)d)) * kLog2e);
   a.tb = L.tb;
   a.n_wg = L.n_wg;
   a.min_share = 128;   // (with 512, six tokens over 4K keys take 34 us instead of 29; with 256, 17 tokens over 600 keys 25 instead of 22)

@@ -77,6 +77,17 @@ def test_rotate_refusals():
     assert S.lib().shadowkv_rope_frequencies(C.byref(inv), FAKE) == S.EINVAL
 
 
+def test_refusals_at_the_ends_of_the_ranges():
+    # a stride that overflows when it is turned into bytes, factors that are finite in 64 bits only, more tokens than a launch has threads for
+    assert rotate(rope(), heads(token_stride=(1 << 62) + 512), heads(data=2 * FAKE)) == S.EINVAL
+    assert rotate(rope(magnitude=1e39), heads(), heads(data=2 * FAKE)) == S.EINVAL and "magnitude" in S.last_error()
+    assert attend(scale=1e39) == S.EINVAL and attend(scale=2.5e38) == S.EINVAL and "softmax_scale" in S.last_error()
+    many = dict(n_tokens=(1 << 27) + 3)
+    assert rotate(rope(), heads(**many), heads(data=2 * FAKE, **many)) == S.EINVAL and "2^27" in S.last_error()
+    k = heads(n_heads=2, token_stride=256, **many)
+    assert append(cache(batch=1), k=k) == S.EINVAL and "2^27" in S.last_error()
+
+
 def test_frequencies():
     f = S.Rope(128, theta=1e4).frequencies()
     assert f.shape == (64,) and f[0] == 1.0 and abs(f[32].item() - 1e-2) < 1e-16
