@@ -124,6 +124,21 @@ def test_other_strides_and_padded_batches(news, layout, dtype):
     assert (out[:4] == 7).all() and (out[4 + t:] == 7).all() and (res[..., 96:] == 7).all()
 
 
+@pytest.mark.parametrize("seqs,hq,hkv,d,dtype", [([(32, 16738)], 14, 2, 64, F8), ([(56, 2527)], 16, 8, 64, BF), ([(1, 60000)], 16, 1, 64, BF),
+                                                  ([(4, 3001), (2, 1200), (5, 4100)], 8, 2, 128, BF), ([(30, 900), (0, 9), (31, 700)], 32, 8, 96, F8),
+                                                  ([(1, 1500 + i) for i in range(40)], 32, 8, 128, BF), ([(8, 33000)], 32, 8, 128, F8)])
+def test_items_shared_by_a_few_or_hundreds_of_workgroups(seqs, hq, hkv, d, dtype):
+    news, lens = [n for n, _ in seqs], [m for _, m in seqs]
+    cache = Cache(lens, hkv, d, dtype, 64, seed=12)
+    q = _q(sum(news), hq, d)
+    out, lse = _attend(cache, q, news)
+    check_attention(cache, q, out, lse, news)
+    for fill in (0, 255):
+        ws = torch.full((S.paged_attention_workspace_bytes(cache.c, hq, sum(news)),), fill, dtype=torch.uint8, device="cuda")
+        again, lse2 = _attend(cache, q, news, workspace=ws)
+        assert torch.equal(again, out) and torch.equal(lse2, lse)
+
+
 def test_equal_runs_need_no_starts_and_results_repeat():
     cache = Cache([300, 17, 2000], 2, 64, BF, 16, seed=3)
     q = _q(12, 8, 64)
