@@ -266,6 +266,8 @@ __device__ __forceinline__ uint2 e5m2x4_to_bf16(uint32_t w) {
 __device__ __forceinline__ bool not_finite(uint32_t w) {
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
+// the same of four E5M2 bytes
+__device__ __forceinline__ bool not_finite_e5m2(uint32_t w) { return ((w & 0x7c7c7c7cu) + 0x04040404u) & 0x80808080u; }
 // the same two with infinities and NaN as zero
 __device__ __forceinline__ uint32_t only_finite(uint32_t w) {
   return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
@@ -429,7 +431,7 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
           const uint32_t w[4] = {stage[j].x, stage[j].y, stage[j].z, stage[j].w};
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            odd |= EB == 2 ? not_finite(w[e]) : (w[e] & 0x7cu) == 0x7cu || (w[e] & 0x7c00u) == 0x7c00u || (w[e] & 0x7c0000u) == 0x7c0000u || (w[e] & 0x7c000000u) == 0x7c000000u;
+            odd |= EB == 2 ? not_finite(w[e]) : not_finite_e5m2(w[e]);
         }
       return odd != 0;
     };
@@ -644,7 +646,7 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
 // written); one of 1M keys, 32/2 heads: 195 us + 14; one of 4K keys: 15 us + 6, a chain of latencies (the share 3, page table and Q 2, keys 3,
 // the merge 2 us).  For 17 to 32 rows the kernel for 128 would take 49 us against 39 (24 chats' drafts, FP8, 14/2 heads of 64), 180
 // against 119 (16 sequences of 16K FP8 keys, 8 tokens each, 32/8 heads of 128), 398 against 351 (bf16, heads of 96, 20 rows), but 219
-// against 226 and 34 against 40 with bf16 heads of 128, whose registers do not hold two blocks of rows: the price of the second term there.
+// against 221 and 34 against 38 with bf16 heads of 128, whose registers do not hold two blocks of rows: the price of the second term there.
 constexpr int kRowsKeys = 32, kRowsNT = 256;
 template <int D>
 struct RowsPitch {
@@ -782,24 +784,28 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
       have = (uint32_t)__ballot(kv.ok);
       request_k();
       const bool mask = t >= clear || h != ~0u;
-      bool odd = false;
+      bool odd = false;   // infinities or NaN among the values of a tile that not all rows see whole
+      if (mask) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+          if (!((h >> ((lane + j * kWave) / kPieces)) & 1)) vr[j] = make_uint4(0, 0, 0, 0);
+          if constexpr (EB == 2) odd |= not_finite(vr[j].x) || not_finite(vr[j].y) || not_finite(vr[j].z) || not_finite(vr[j].w);
+          else odd |= not_finite_e5m2(vr[j].x) || not_finite_e5m2(vr[j].y) || not_finite_e5m2(vr[j].z) || not_finite_e5m2(vr[j].w);
+        }
+        odd = __any(odd);
+      }
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         const int p = lane + j * kWave, r = p / kPieces, c = p - r * kPieces;
-        uint4 v = vr[j];
-        if (h != ~0u && !((h >> r) & 1)) v = make_uint4(0, 0, 0, 0);
+        const uint4 v = vr[j];
         if constexpr (EB == 2) {
           *reinterpret_cast<uint4*>(mine + r * PV + c * 16) = v;
-          if (mask) odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
         } else {
           const uint2 v0 = e5m2x4_to_bf16(v.x), v1 = e5m2x4_to_bf16(v.y), v2 = e5m2x4_to_bf16(v.z), v3 = e5m2x4_to_bf16(v.w);
           *reinterpret_cast<uint4*>(mine + r * PV + c * 32) = make_uint4(v0.x, v0.y, v1.x, v1.y);
           *reinterpret_cast<uint4*>(mine + r * PV + c * 32 + 16) = make_uint4(v2.x, v2.y, v3.x, v3.y);
-          if (mask) odd |= not_finite(v0.x) || not_finite(v0.y) || not_finite(v1.x) || not_finite(v1.y) || not_finite(v2.x) ||
-                           not_finite(v2.y) || not_finite(v3.x) || not_finite(v3.y);
         }
       }
-      odd = __any(odd);
       request_v();
       page = lookup(t + 2 * NW);
       uint32_t ph[NB][4], pl[NB][4];
@@ -839,21 +845,7 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
       // V in the wave's LDS: written above by other lanes
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      const uint8_t* vp = mine + (4 * quarter + (col >> 2)) * PV + (col & 3) * 8;
-#pragma unroll
-      for (int i = 0; i < DB; ++i) {
-        uint2 x = read_tr(vp + i * 32), y = read_tr(vp + 16 * PV + i * 32);
-        if (odd) x = make_uint2(only_finite(x.x), only_finite(x.y)), y = make_uint2(only_finite(y.x), only_finite(y.y));
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y));
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, make_uint4(ph[n][0], ph[n][1], ph[n][2], ph[n][3])),
-                                                            o[n][i], 0, 0, 0);
-          o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, make_uint4(pl[n][0], pl[n][1], pl[n][2], pl[n][3])),
-                                                            o[n][i], 0, 0, 0);
-        }
-      }
-      if (odd) {
+      if (odd) {   // they go to the rows that see their keys, and are zero for the product (a weight of zero does not make them harmless)
         for (int k = 0; k < kRowsKeys; ++k) {
           if (!((h >> k) & 1)) continue;
 #pragma unroll
@@ -866,6 +858,27 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
               for (int n = 0; n < NB; ++n)
                 if (t * kRowsKeys + k <= limit[n] && (__float_as_uint(e[j]) & 0x7f800000u) == 0x7f800000u) o[n][i][j] += e[j];
           }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        for (int j = lane; j < kRowsKeys * D / 4; j += kWave) {
+          uint2* w = reinterpret_cast<uint2*>(mine + j / (D / 4) * PV + j % (D / 4) * 8);
+          *w = make_uint2(only_finite(w->x), only_finite(w->y));
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+      const uint8_t* vp = mine + (4 * quarter + (col >> 2)) * PV + (col & 3) * 8;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) {
+        const uint2 x = read_tr(vp + i * 32), y = read_tr(vp + 16 * PV + i * 32);
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y));
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, make_uint4(ph[n][0], ph[n][1], ph[n][2], ph[n][3])),
+                                                            o[n][i], 0, 0, 0);
+          o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, make_uint4(pl[n][0], pl[n][1], pl[n][2], pl[n][3])),
+                                                            o[n][i], 0, 0, 0);
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
