@@ -28,22 +28,26 @@ struct Joined {   // a row's state as parts are added
 // All is latency: one load and a vote find the parts, eight of them are requested at a time.
 // The rows of an item are shared by the workgroups whose like worked at it.  Where it has few parts each group joins a
 // row of its own, half of the groups for the item that began here and half for the one that goes on or ends here; where it has
-// more, the groups share the parts of a row.  6 us for 31 parts of 4 rows, 13 us for some ten parts each of 60 ragged items of up to 32
-// rows, 5 us behind a prompt of 8K tokens; 3 us of that go into finding the parts.
-constexpr int kFewParts = 16;
+// more, the groups share the parts of a row.  5 us for 31 parts of 4 rows, 11 us for some ten parts each of 60 ragged items of up to 32
+// rows, 5 us behind a prompt of 8K tokens; 3 us of that go into finding the parts.  256 threads for up to 32 rows (with 512 the first
+// two took 6 and 13, with 128 the 256 parts of a token over 1M keys 22 instead of 15), 512 for 128 rows (1024: 34 us against 28 for 32 tokens
+// over 16.7K keys on 14/2 heads, the whole call).
+constexpr int kFewParts = 16, kMaxWg = 512;
 template <int NT>
 __global__ __launch_bounds__(NT) void paged_attn_join_kernel(PagedAttnArgs a, int block_rows) {
-  static_assert(NT >= 512);   // (a thread per workgroup of the first kernel)
-  constexpr int kGroups = NT / 32, kHalf = kGroups / 2, kAhead = 8, kWords = NT / kWave;
+  static_assert(kMaxWg % NT == 0);
+  constexpr int kGroups = NT / 32, kHalf = kGroups / 2, kAhead = 8, kWords = kMaxWg / kWave;
   __shared__ float acc_s[kGroups][128];
   __shared__ float2 ml_s[kGroups];
   __shared__ uint64_t tails[kWords], heads[kWords], lasts[kWords];
   const int me = blockIdx.x, tid = threadIdx.x, grp = tid >> 5, c = (tid & 31) * 4, col = min(c, a.d - 4);
-  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), flags = tid < a.n_wg ? a.desc[tid].x : 0;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), n = a.n_wg;
   const int4 mine = a.desc[me];
-  {
+#pragma unroll
+  for (int i0 = 0; i0 < kMaxWg; i0 += NT) {
+    const int i = i0 + tid, flags = i < n ? a.desc[i].x : 0;
     const uint64_t t = __ballot(flags & kPartTail), h = __ballot(flags & kPartHead), l = __ballot(flags & kPartLast);
-    if (tid % kWave == 0) { tails[tid / kWave] = t; heads[tid / kWave] = h; lasts[tid / kWave] = l; }
+    if (tid % kWave == 0) { tails[i / kWave] = t; heads[i / kWave] = h; lasts[i / kWave] = l; }
   }
   __syncthreads();
   auto end_of = [&](int w) {   // the first behind w that finished an item
@@ -111,7 +115,7 @@ __global__ __launch_bounds__(NT) void paged_attn_join_kernel(PagedAttnArgs a, in
     else if (it.parts <= 4) go(std::integral_constant<int, 2>{});
     else go(std::integral_constant<int, 1>{});
   };
-  if (wave < kWords / 2) join_few(own, true);
+  if (wave < NT / kWave / 2) join_few(own, true);
   else join_few(around, false);
   auto join_many = [&](const Item& it) {
     if (few(it)) return;
@@ -137,13 +141,13 @@ __global__ __launch_bounds__(NT) void paged_attn_join_kernel(PagedAttnArgs a, in
 
 // (up to 32 rows the kernel that reads keys fastest and weighs in two terms, else the one with the most products per byte read)
 int paged_attn_block_rows(int G, long rows) { return G <= 16 && rows <= 16 ? 16 : G <= 32 && rows <= 32 ? 32 : kTileRows; }
-int paged_attn_workgroups(int block_rows) { return 512; }   // two per compute unit; a multiple of eight, and at most 512 (the join)
+int paged_attn_workgroups(int block_rows) { return kMaxWg; }   // two per compute unit; a multiple of eight
 
 hipError_t launch_paged_attention(PagedAttnArgs a, int block_rows, hipStream_t st) {
   hipError_t e = a.kv_bytes == 1 ? launch_paged_attn_fp8(a, block_rows, st) : launch_paged_attn_eb<2>(a, block_rows, st);
   if (e != hipSuccess) return e;
-  if (block_rows == kTileRows) hipLaunchKernelGGL(paged_attn_join_kernel<1024>, dim3(a.n_wg), dim3(1024), 0, st, a, block_rows);
-  else hipLaunchKernelGGL(paged_attn_join_kernel<512>, dim3(a.n_wg), dim3(512), 0, st, a, block_rows);
+  if (block_rows == kTileRows) hipLaunchKernelGGL(paged_attn_join_kernel<512>, dim3(a.n_wg), dim3(512), 0, st, a, block_rows);
+  else hipLaunchKernelGGL(paged_attn_join_kernel<256>, dim3(a.n_wg), dim3(256), 0, st, a, block_rows);
   return hipGetLastError();
 }
 

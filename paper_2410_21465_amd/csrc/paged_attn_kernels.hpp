@@ -642,9 +642,9 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
 // the product is free as long as Q's is the same.  V goes through a piece of LDS of the wave's own, so nothing waits for
 // another wave before the end.  The next 32 keys are requested as soon as the registers are free.  The softmax weights enter as two bf16 terms:
 // the matrix pipe has the time (32 keys of two waves take a SIMD's 0.3 us, and their bytes 6 us at 5.2 TB/s).
-// 16 sequences of 32K keys, a token each, 32/8 heads of 128: 243 us + 6 for the join, 5.5 TB/s (a large copy: 5.0 to 5.4, read and
-// written); one of 1M keys, 32/2 heads: 195 us + 14; one of 4K keys: 15 us + 6, a chain of latencies (the share 3, page table and Q 2, keys 3,
-// the merge 2 us).  For 17 to 32 rows the kernel for 128 would take 49 us against 39 (24 chats' drafts, FP8, 14/2 heads of 64), 180
+// 16 sequences of 32K keys, a token each, 32/8 heads of 128: 237 us + 6 for the join, 5.5 TB/s (a large copy: 5.0 to 5.4, read and
+// written); one of 1M keys, 32/2 heads: 191 us + 13; one of 4K keys: 14 us + 5, a chain of latencies (the share 3, page table and Q 2, keys 3,
+// the merge 2 us).  For 17 to 32 rows the kernel for 128 would take 49 us against 37 (24 chats' drafts, FP8, 14/2 heads of 64), 180
 // against 119 (16 sequences of 16K FP8 keys, 8 tokens each, 32/8 heads of 128), 398 against 351 (bf16, heads of 96, 20 rows), but 219
 // against 221 and 34 against 38 with bf16 heads of 128, whose registers do not hold two blocks of rows: the price of the second term there.
 constexpr int kRowsKeys = 32, kRowsNT = 256;
