@@ -250,7 +250,7 @@ struct PagedAttnArgs {
   int min_share;            // least work of a workgroup, in keys
   int4* desc;               // [n_wg] flags of the items that a workgroup leaves unfinished; of its last one first token, KV head and rows
   float* part_acc;          // [2 n_wg, block rows, d] unnormalised sums
-  float2* part_ml;          // [2 n_wg, block rows] (max in log2 units, sum)
+  float2* part_ml;          // [2 n_wg, block rows] (reference of the logits in log2 units, sum)
 };
 // Rows (tokens x query heads per KV head) of a row block: 16 or 32 where a workgroup's waves share out the keys, 128 where
 // they share out the rows.  rows: what a sequence has on average.

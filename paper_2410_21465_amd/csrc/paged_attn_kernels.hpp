@@ -1,8 +1,12 @@
 // Attention of new tokens over a paged cache (shadowkv_paged_attention):
 //   out = sum over the places l a row sees of softmax_l(scale <q, k_l>) v_l.
 // A row is one (token, query head); the G = h_q / h_kv rows of a token that share a KV head lie side by side in a block of rows, so
-// that K and V are read once for all of them.  One pass over the keys with a running maximum m and sum l in fp32 (log2 units):
-// a tile's logits S, m' = max(m, S), P = 2^(S - m'), l' = l 2^(m - m') + sum P, O' = O 2^(m - m') + P V, out = O / l.
+// that K and V are read once for all of them.  One pass over the keys with a reference m of the logits and a running sum l in fp32
+// (log2 units): a tile's logits S, P = 2^(S - m), l' = l + sum P, O' = O + P V, out = O / l, lse = m + log l.  Where a logit passes m, m
+// moves 2^8 beyond the largest one (l and O by the same factor), so that it seldom moves and no weight ever passes one: P V overflows
+// only where the softmax with its maximum taken out would too.  (With m at the maximum, and weights of up to 2^8 let through before it
+// moves, which is the same arithmetic 2^8 higher up, finite values from 2^120 on came out infinite.)  The largest weight lies in
+// [2^-8, 1]; weights and sums are fp32, whose exponents have room for that at the lower end: bf16's smallest values come out exact.
 //
 // Both kernels form S^T = K Q^T, so that a lane of the matrix instruction's result holds one row's logits: the maximum
 // and the sum stay in the lane but for one exchange, the factors of a row are scalars of its lane, and P^T is already laid out as
@@ -294,6 +298,7 @@ __device__ __forceinline__ float sum_quarters(float x) {
   return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kHeadroom = 8.f;   // how far beyond the largest logit the reference of a row moves, in powers of two
 
 // Where a key's rows lie: offsets of its K and V rows (head excluded) in 16-byte units (the host sees to it that they fit).  Keys
 // without a row get the cache's first one (in bounds; what is read there is masked out) and ok = false.
@@ -531,9 +536,8 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
       };
       read_values(0, vf[0]);   // arrives while the weights are formed
       top = max_halves(top) * a.scale_log2;
-      // The maximum follows the logits only where they pass it by 2^8: weights up to that lose nothing in bf16 or in fp32 sums.
-      if (__any(top > m + 8.f)) {
-        const float next_m = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next_m);
+      if (__any(top > m)) {
+        const float next_m = fmaxf(m, top + kHeadroom), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next_m);
         m = next_m;
         l *= f;
 #pragma unroll
@@ -822,8 +826,8 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
 #pragma unroll
         for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
         top = max_quarters(top);
-        if (__any(top > m[n] + 8.f)) {
-          const float next = fmaxf(m[n], top), f = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - next);
+        if (__any(top > m[n])) {
+          const float next = fmaxf(m[n], top + kHeadroom), f = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - next);
           m[n] = next;
           l[n] *= f;
 #pragma unroll
