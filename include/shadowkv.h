@@ -421,7 +421,8 @@ int shadowkv_paged_append(const shadowkv_paged_cache *cache, const shadowkv_rope
  * where it sees l <= kv_lens[i] - n_i + j with causal != 0, else every l < kv_lens[i].  kv_lens is held to
  * [0, pages_per_seq * page_size].  What a token does not see (later tokens, entries without a page, rows behind the
  * length) has no influence on it, whatever is stored there, NaN and infinities among it.  A token that sees nothing, or whose logits
- * are all minus infinity, gets out = 0 and lse = -inf.
+ * are all minus infinity, gets out = 0 and lse = -inf.  An infinite value that a token does see makes its element infinite; NaN where
+ * infinities of both signs meet, and possibly where its weight is less than 2^-90 of the largest.
  *
  *   q, out     [1, T, h_q, d] bf16; h_q / h_kv <= 64; rows outside every run are left as they were
  *   lse        dev out [T, h_q] fp32 or NULL: natural logarithm of the sum of exp(scale <q, k_l>)

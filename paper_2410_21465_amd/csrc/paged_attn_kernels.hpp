@@ -840,8 +840,9 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
         for (int j = 0; j < 8; j += 2) {
           const float p0 = __builtin_amdgcn_exp2f(x[j] - mm), p1 = __builtin_amdgcn_exp2f(x[j + 1] - mm);
           l[n] += p0 + p1;
-          // the upper halves, and what they leave out (exact), rounded
-          const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+          // the upper halves, and what they leave out (exact), rounded.  Taken from the number below, so that no weight but zero leaves
+          // nothing out: zero times an infinite value would be NaN.
+          const uint32_t u0 = __builtin_elementwise_sub_sat(__float_as_uint(p0), 1u), u1 = __builtin_elementwise_sub_sat(__float_as_uint(p1), 1u);
           ph[n][j >> 1] = upper_halves(u0, u1);
           pl[n][j >> 1] = pack_bf16(p0 - __uint_as_float(u0 & 0xffff0000u), p1 - __uint_as_float(u1 & 0xffff0000u));
         }
