@@ -620,6 +620,13 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
     l = sum_halves(l);
     if (slot < 0) {
       if (!row_ok) return;
+      // (no weight at all: zero, whatever infinite values made of o)
+      if (l == 0.f) {
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+      }
       const float f = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
       uint8_t* dst = a.out.p + qrow * a.out.tok + (head * G + g) * a.out.head + half * 8;
 #pragma unroll

@@ -42,3 +42,21 @@ def test_an_infinite_value_in_a_tile_that_all_rows_see(n, d, hq, bad, equal, dty
         assert (out[:, hq // 2:, e].float() == bad).all()
     rest = [e for e in range(d) if e not in (5, d - 1)]
     assert torch.equal(out[:, hq // 2:, rest], clean[:, hq // 2:, rest])
+
+
+@pytest.mark.parametrize("n,L", [(1, 64), (4, 300), (40, 64), (40, 1000), (40, 61)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_logits_of_minus_infinity_throughout(n, L, causal):
+    """Such a token gets zeros and a log-sum of minus infinity, infinite values or not."""
+    cache = Cache([L, L], 2, 128, BF, 16, seed=6)
+    k = cache.kd[0].to(BF)
+    k[..., 0] = -math.inf
+    v = cache.vd[0].to(BF)
+    v[3, :, 7] = math.inf
+    v[L - n, :, 8] = math.nan
+    cache.put(0, k, v)
+    q = _q(2 * n, 8, 128)
+    q[..., 0] = 1.0
+    out, lse = _attend(cache, q, [n, n], causal=causal)
+    assert (out[:n] == 0).all() and (lse[:n] == -math.inf).all()
+    assert torch.isfinite(out[n:].float()).all() and torch.isfinite(lse[n:]).all()
