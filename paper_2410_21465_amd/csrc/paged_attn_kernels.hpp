@@ -921,8 +921,8 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
         const float2 ml = mml[w * BR + row];
+        if (ml.x == -INFINITY && ml.y == 0.f) continue;   // (no weight at all)
         const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
-        if (f == 0.f && ml.y == ml.y) continue;
         const float4 v = *reinterpret_cast<const float4*>(macc + (w * BR + row) * D + c);
         sum += ml.y * f;
         x[0] += v.x * f; x[1] += v.y * f; x[2] += v.z * f; x[3] += v.w * f;

@@ -60,3 +60,22 @@ def test_logits_of_minus_infinity_throughout(n, L, causal):
     out, lse = _attend(cache, q, [n, n], causal=causal)
     assert (out[:n] == 0).all() and (lse[:n] == -math.inf).all()
     assert torch.isfinite(out[n:].float()).all() and torch.isfinite(lse[n:]).all()
+
+
+@pytest.mark.parametrize("n", [1, 4, 40])
+def test_an_infinite_value_is_not_lost_where_its_weight_is(n):
+    """A key whose weight lies below fp32's range, and so do those of every fourth run of 32 keys with it: its infinite value does not come
+    out as a finite one, wherever it stands."""
+    L, d = 260, 64
+    for at in (2, 40, 70, 100, 130, 250):
+        cache = Cache([L], 1, d, BF, 16, seed=7)
+        k = torch.zeros(L, 1, d, device="cuda")
+        k[torch.arange(L, device="cuda") // 32 % 4 == at // 32 % 4, 0, 0] = -400.0
+        v = cache.vd[0].to(BF)
+        v[at, 0, 9] = math.inf
+        cache.put(0, k.to(BF), v)
+        q = torch.zeros(n, 4, d, dtype=BF, device="cuda")
+        q[..., 0] = 1.0
+        out, _ = _attend(cache, q, [n], softmax_scale=math.log(2.0), causal=False)
+        assert not torch.isfinite(out[..., 9].float()).any(), f"key {at}"
+        assert torch.isfinite(out[..., 10:].float()).all() and torch.isfinite(out[..., :9].float()).all(), f"key {at}"
