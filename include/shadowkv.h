@@ -427,7 +427,7 @@ int shadowkv_paged_append(const shadowkv_paged_cache *cache, const shadowkv_rope
  *   q, out     [1, T, h_q, d] bf16; h_q / h_kv <= 64; rows outside every run are left as they were
  *   lse        dev out [T, h_q] fp32 or NULL: natural logarithm of the sum of exp(scale <q, k_l>)
  *   seq_starts, kv_lens  as shadowkv_paged_append
- *   softmax_scale  0 => 1/sqrt(d)
+ *   softmax_scale  0 => 1/sqrt(d); else times log2(e) a normal positive fp32 number, 8.15e-39 ... 2.35e38
  *   workspace  dev >= shadowkv_paged_attention_workspace_bytes(), 256-byte aligned; its contents do not matter.  Two
  *              calls whose work may overlap need a workspace each.
  * Products and sums are fp32; the softmax weights are rounded to bf16 for the product with the values where a call has more than

@@ -1,6 +1,7 @@
 // C ABI of rotary positions and the paged cache (see include/shadowkv.h): argument checks, and what the kernels are handed.
 // Nothing here touches the GPU before the arguments have been accepted.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "api.hpp"
@@ -287,7 +288,9 @@ int shadowkv_paged_attention(const shadowkv_paged_cache* cache, const shadowkv_h
   if (q->n_seqs != 1 || out->n_seqs != 1) return fail_inval("q and out are one run of tokens: n_seqs must be 1");
   if (q->n_tokens != out->n_tokens || q->n_heads != out->n_heads) return fail_inval("q and out differ in size");
   if (q->dtype != SHADOWKV_KV_BF16 || out->dtype != SHADOWKV_KV_BF16) return fail_inval("q and out must be bf16");
-  if (!(softmax_scale >= 0.0) || !std::isfinite((float)(softmax_scale * kLog2e))) return fail_inval("softmax_scale must be finite (in fp32) and >= 0");
+  const float scale_log2 = (float)((softmax_scale != 0.0 ? softmax_scale : 1.0 / std::sqrt((double)d)) * kLog2e);
+  // (below: no scale at all, and a hidden logit of minus infinity times zero would be NaN)
+  if (!(scale_log2 >= FLT_MIN) || !std::isfinite(scale_log2)) return fail_inval("softmax_scale must be 0, or positive and a normal number in fp32 when multiplied by log2(e)");
   rc = check_runs(cache, q, seq_starts, kv_lens);
   if (rc != SHADOWKV_OK) return rc;
   PagedAttnLayout L;
@@ -306,7 +309,7 @@ int shadowkv_paged_attention(const shadowkv_paged_cache* cache, const shadowkv_h
   a.pt = table_arg(cache);
   a.runs = RunsArg{seq_starts, kv_lens, cache->batch, q->n_tokens};
   a.hq = q->n_heads; a.hkv = cache->n_kv_heads; a.G = L.G; a.d = d; a.kv_bytes = eb; a.causal = causal != 0;
-  a.scale_log2 = (float)((softmax_scale != 0.0 ? softmax_scale : 1.0 / std::sqrt((double)d)) * kLog2e);
+  a.scale_log2 = scale_log2;
   a.tb = L.tb;
   a.n_wg = L.n_wg;
   a.min_share = 128;   // (with 512, six tokens over 4K keys take 34 us instead of 29; with 256, 17 tokens over 600 keys 25 instead of 22)

@@ -49,3 +49,13 @@ def test_the_smallest_values_keep_their_bits(n):
     out = S.paged_attention(cache.c, q, cache.kv_lens())
     # off by the weights' rounding (a 2^-8 of at most 7 steps), then by half a step of the result's
     assert ((out.double() - row.double()).abs() <= (0.5 + 7 * 2.0 ** -7) * 2.0 ** -133).all()
+
+
+@pytest.mark.parametrize("scale", [8.2e-39, 1e-30])
+@pytest.mark.parametrize("n", [1, 70])
+def test_the_smallest_scales_give_means(n, scale):
+    cache = Cache([300, 90], 2, 96, F8, 16, seed=5, k_gain=8.0)
+    q = torch.randn(2 * n, 8, 96, generator=torch.Generator(device="cuda").manual_seed(6), device="cuda").to(BF)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    out = S.paged_attention(cache.c, q, cache.kv_lens(), seq_starts=cache.starts([n, n]), softmax_scale=scale, lse=lse)
+    check_attention(cache, q, out, lse, [n, n], scale=scale)
