@@ -18,17 +18,20 @@ int elem_bytes(int dtype) { return dtype == SHADOWKV_KV_FP8_E5M2 ? 1 : 2; }
 bool known_dtype(int dtype) { return dtype == SHADOWKV_KV_BF16 || dtype == SHADOWKV_KV_FP8_E5M2; }
 bool known_head_dim(int d) { return d == 64 || d == 96 || d == 128; }
 
-// Strides of dimensions of these sizes, innermost rows of `row` elements: multiples of 16 bytes, and not negative; of an array that is
-// written no two rows may overlap.
+// Strides of dimensions of these sizes, innermost rows of `row` elements: multiples of 16 bytes, and not negative, in all within what can
+// be addressed; of an array that is written no two rows may overlap.
 int check_strides(const char* name, const int64_t* stride, const int64_t* size, int n, int64_t row, int eb, bool written) {
   int64_t st[3], sz[3];
   int k = 0;
+  double span = 0.0;
   for (int i = 0; i < n; ++i) {
     if (size[i] <= 1) continue;
+    span += (double)stride[i] * (double)(size[i] - 1);
     if (stride[i] < 0 || stride[i] > ((int64_t)1 << 48) || stride[i] * eb % 16)
       return fail_inval("%s: strides must be multiples of 16 bytes and not negative", name);
     st[k] = stride[i]; sz[k] = size[i]; ++k;
   }
+  if (span * eb > 281474976710656.0) return fail_inval("%s: the strides span more than 2^48 bytes", name);
   if (!written) return SHADOWKV_OK;
   for (int i = 1; i < k; ++i)
     for (int j = i; j > 0 && st[j] < st[j - 1]; --j) { std::swap(st[j], st[j - 1]); std::swap(sz[j], sz[j - 1]); }

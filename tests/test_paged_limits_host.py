@@ -11,3 +11,9 @@ def test_softmax_scales_that_vanish_in_fp32():
         assert attend(scale=scale) == S.EINVAL and "softmax_scale" in S.last_error()
     for scale in (0.0, 8.2e-39, 1e-30):
         assert attend(scale=scale, ws=None) == S.EWORKSPACE          # (accepted: the workspace is looked at next)
+
+
+def test_arrays_that_span_more_than_there_is():
+    for big in (dict(token_stride=1 << 47), dict(head_stride=1 << 46), dict(n_seqs=1 << 12, seq_stride=1 << 40, n_tokens=1)):
+        assert rotate(rope(), heads(**big), heads(data=2 * FAKE)) == S.EINVAL and "span" in S.last_error(), S.last_error()
+        assert rotate(rope(), heads(data=2 * FAKE), heads(**big)) == S.EINVAL and "span" in S.last_error()
