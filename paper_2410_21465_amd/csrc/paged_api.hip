@@ -60,9 +60,10 @@ HeadsArg heads_arg(const shadowkv_heads* h) {
   return {static_cast<uint8_t*>(h->data), h->seq_stride * eb, h->token_stride * eb, h->head_stride * eb, eb};
 }
 
+// (of equal sizes; the stride of a dimension of one says nothing)
 bool same_array(const shadowkv_heads* a, const shadowkv_heads* b) {
-  return a->data == b->data && a->dtype == b->dtype && a->seq_stride == b->seq_stride && a->token_stride == b->token_stride &&
-         a->head_stride == b->head_stride;
+  return a->data == b->data && a->dtype == b->dtype && (a->n_seqs <= 1 || a->seq_stride == b->seq_stride) &&
+         (a->n_tokens <= 1 || a->token_stride == b->token_stride) && (a->n_heads <= 1 || a->head_stride == b->head_stride);
 }
 
 // Whether [a, a + extent) and [b, b + extent) share memory.
