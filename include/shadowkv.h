@@ -317,8 +317,9 @@ size_t shadowkv_argtopk_workspace_bytes(int32_t units, int32_t n, int32_t k);
  *
  * Arrays of heads, [n_seqs, n_tokens, n_heads, d], are handed over with their strides (in elements); the d elements of
  * a head are contiguous.  Pointers, and strides of dimensions longer than one, are multiples of 16 bytes, and no stride
- * is negative.  An array that is written may not overlap itself or, unless a call says so, any other argument.  Ragged runs of
- * tokens are one sequence of n_tokens = T tokens, cut by seq_starts.
+ * is negative.  An array that is written may not overlap itself or, unless a call says so, any other argument (it is refused where its
+ * first or last head lies in the array that it is made of, or the other way round; arrays that only interleave do not overlap).
+ * Ragged runs of tokens are one sequence of n_tokens = T tokens, cut by seq_starts.
  */
 typedef struct shadowkv_heads {
   void *data;                                    /* dev */

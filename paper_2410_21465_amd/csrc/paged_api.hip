@@ -66,10 +66,37 @@ bool same_array(const shadowkv_heads* a, const shadowkv_heads* b) {
          (a->n_tokens <= 1 || a->token_stride == b->token_stride) && (a->n_heads <= 1 || a->head_stride == b->head_stride);
 }
 
-// Whether [a, a + extent) and [b, b + extent) share memory.
-int64_t extent_bytes(const shadowkv_heads* h, int d) {
-  return ((int64_t)(h->n_seqs - 1) * h->seq_stride + (int64_t)(h->n_tokens - 1) * h->token_stride + (int64_t)(h->n_heads - 1) * h->head_stride + d) *
-         elem_bytes(h->dtype);
+// The bytes of an array of heads, as nested loops over its rows with the widest stride outside.
+struct Rows {
+  const char* p;
+  int64_t st[3], sz[3], row, last;   // last: where the last row begins, from p
+  Rows(const shadowkv_heads* h, int d) : p(static_cast<const char*>(h->data)) {
+    const int eb = elem_bytes(h->dtype);
+    const int64_t s[3] = {h->seq_stride, h->token_stride, h->head_stride}, n[3] = {h->n_seqs, h->n_tokens, h->n_heads};
+    row = (int64_t)d * eb;
+    last = 0;
+    for (int i = 0; i < 3; ++i) { st[i] = n[i] > 1 ? s[i] * eb : 0; sz[i] = n[i]; last += st[i] * (n[i] - 1); }
+    for (int i = 1; i < 3; ++i)
+      for (int j = i; j > 0 && st[j] > st[j - 1]; --j) { std::swap(st[j], st[j - 1]); std::swap(sz[j], sz[j - 1]); }
+  }
+  bool holds(const char* at) const {   // whether a row that this finds holds the byte
+    int64_t off = at - p;
+    if (off < 0 || off >= last + row) return false;
+    for (int i = 0; i < 3; ++i)
+      if (st[i] > 0) off -= std::min(off / st[i], sz[i] - 1) * st[i];
+    return off < row;
+  }
+  bool holds_ends(const Rows& o) const { return holds(o.p) || holds(o.p + o.row - 1) || holds(o.p + o.last) || holds(o.p + o.last + o.row - 1); }
+};
+// Whether the first or the last row of one array lies in the other, so that arrays are refused that begin or end inside each other and
+// those that only interleave are not.
+bool share_memory(const shadowkv_heads* a, const shadowkv_heads* b, int d) {
+  const Rows x(a, d), y(b, d);
+  return x.p < y.p + y.last + y.row && y.p < x.p + x.last + x.row && (x.holds_ends(y) || y.holds_ends(x));
+}
+int check_apart(const char* read, const shadowkv_heads* a, const char* written, const shadowkv_heads* b, int d) {
+  if (a->n_seqs == 0 || a->n_tokens == 0 || same_array(a, b) || !share_memory(a, b, d)) return SHADOWKV_OK;
+  return fail_inval("%s and %s share memory and are laid out differently", read, written);
 }
 
 int rope_table(const shadowkv_rope* r, double* w) {   // radians per position
@@ -223,12 +250,9 @@ int shadowkv_rotate(const shadowkv_rope* rope, const shadowkv_heads* x, const sh
   if (x->n_seqs != out->n_seqs || x->n_tokens != out->n_tokens || x->n_heads != out->n_heads) return fail_inval("x and out differ in size");
   if (positions && pos_offset) return fail_inval("positions and pos_offset exclude each other");
   if ((int64_t)x->n_seqs * x->n_tokens > kMaxLaunchTokens) return fail_inval("more than 2^27 tokens");
+  rc = check_apart("x", x, "out", out, rope->head_dim);
+  if (rc != SHADOWKV_OK) return rc;
   if (x->n_seqs == 0 || x->n_tokens == 0) return SHADOWKV_OK;
-  if (!same_array(x, out)) {
-    const char *a = static_cast<const char*>(x->data), *b = static_cast<const char*>(out->data);
-    if (a < b + extent_bytes(out, rope->head_dim) && b < a + extent_bytes(x, rope->head_dim) && x->data == out->data)
-      return fail_inval("out begins where x does and is laid out differently");
-  }
   const hipError_t e = launch_rotate(rope_args(rope, w, transposed != 0), heads_arg(x), heads_arg(out), positions, pos_offset, x->n_seqs, x->n_tokens,
                                      x->n_heads, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SHADOWKV_OK : fail_hip("rotate", e);
@@ -262,6 +286,8 @@ int shadowkv_paged_append(const shadowkv_paged_cache* cache, const shadowkv_rope
   rc = check_runs(cache, k, seq_starts, kv_lens);
   if (rc != SHADOWKV_OK) return rc;
   if (k->n_tokens > kMaxLaunchTokens) return fail_inval("more than 2^27 tokens");
+  if (q) rc = check_apart("q", q, "q_out", q_out, d);
+  if (rc != SHADOWKV_OK) return rc;
   if (k->n_tokens == 0) return SHADOWKV_OK;
   const int eb = elem_bytes(cache->kv_dtype);
   RopeArgs ra{};
@@ -299,6 +325,7 @@ int shadowkv_paged_attention(const shadowkv_paged_cache* cache, const shadowkv_h
   if (rc != SHADOWKV_OK) return rc;
   PagedAttnLayout L;
   rc = paged_attn_layout(cache, q->n_heads, q->n_tokens, &L);
+  if (rc == SHADOWKV_OK) rc = check_apart("q", q, "out", out, d);
   if (rc == SHADOWKV_OK) rc = check_workspace(workspace, workspace_bytes, L.total);
   if (rc != SHADOWKV_OK) return rc;
   if (q->n_tokens == 0) return SHADOWKV_OK;

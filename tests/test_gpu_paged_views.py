@@ -22,3 +22,23 @@ def test_in_place_through_two_views_of_one_token():
     off = torch.arange(100, 105, dtype=torch.int32, device="cuda")
     assert S.rotate(r, x, out=out, pos_offset=off) is out
     check_turned(r, out, was, off[:, None])
+
+
+def test_heads_of_one_projection_beside_each_other():
+    """q, k and v of one array, q rotated into every other head of another, and out of attention beside its q."""
+    t, hq, hkv, d = 40, 8, 2, 64
+    qkv = _x(2, t, hq + 2 * hkv, d)
+    cache = Cache([0], hkv, d, BF, 16, spare=3, width=3)
+    cache.table_cpu = torch.arange(3, dtype=torch.int32)[None]
+    c = S.PagedCache(cache.k, cache.v, cache.table_cpu.cuda())
+    lens = torch.tensor([t], dtype=torch.int32, device="cuda")
+    both = torch.zeros(t, 2 * hq, d, dtype=BF, device="cuda")
+    r = S.Rope(d)
+    q, k, v = qkv.split([hq, hkv, hkv], 1)
+    want = S.paged_append(c, k, v, lens, rope=r, q=q)
+    S.paged_append(c, k, v, lens, rope=r, q=q, q_out=both[:, ::2])
+    assert torch.equal(both[:, ::2], want) and (both[:, 1::2] == 0).all()
+    S.paged_attention(c, both[:, ::2], lens, out=both[:, 1::2])
+    assert torch.equal(both[:, 1::2], S.paged_attention(c, want, lens)) and torch.equal(both[:, ::2], want)
+    with pytest.raises(S.ShadowKVError, match="share memory"):
+        S.paged_append(c, k[:-1], v[:-1], lens, rope=r, q=q[:-1], q_out=q[1:])
