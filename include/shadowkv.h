@@ -425,7 +425,7 @@ int shadowkv_paged_append(const shadowkv_paged_cache *cache, const shadowkv_rope
  * are all minus infinity, gets out = 0 and lse = -inf.  An infinite value that a token does see makes its element infinite; NaN where
  * infinities of both signs meet, and possibly where its weight is less than 2^-90 of the largest.
  *
- *   q, out     [1, T, h_q, d] bf16; h_q / h_kv <= 64; rows outside every run are left as they were
+ *   q, out     [1, T, h_q, d] bf16, T <= 2^30; h_q / h_kv <= 64; rows outside every run are left as they were
  *   lse        dev out [T, h_q] fp32 or NULL: natural logarithm of the sum of exp(scale <q, k_l>)
  *   seq_starts, kv_lens  as shadowkv_paged_append
  *   softmax_scale  0 => 1/sqrt(d); else times log2(e) a normal positive fp32 number, 8.15e-39 ... 2.35e38

@@ -12,6 +12,7 @@ using namespace skv;
 namespace {
 
 constexpr double kLog2e = 1.4426950408889634074;
+constexpr int64_t kMaxSeqTokens = (int64_t)1 << 30;      // of a sequence in the cache
 constexpr int64_t kMaxLaunchTokens = (int64_t)1 << 27;   // of a launch with up to 16 threads a token: 2^31 threads
 
 int elem_bytes(int dtype) { return dtype == SHADOWKV_KV_FP8_E5M2 ? 1 : 2; }
@@ -170,7 +171,7 @@ int check_cache(const shadowkv_paged_cache* c, bool pointers, bool written) {
   if (!known_head_dim(c->head_dim)) return fail_inval("head_dim must be 64, 96 or 128");
   if (c->page_size < 1 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)))
     return fail_inval("page_size must be a power of two in [1, 65536]");
-  if ((int64_t)c->pages_per_seq * c->page_size > ((int64_t)1 << 30)) return fail_inval("more than 2^30 tokens a sequence");
+  if ((int64_t)c->pages_per_seq * c->page_size > kMaxSeqTokens) return fail_inval("more than 2^30 tokens a sequence");
   if (!known_dtype(c->kv_dtype)) return fail_inval("kv_dtype must be SHADOWKV_KV_BF16 or SHADOWKV_KV_FP8_E5M2");
   if (c->reserved) return fail_inval("reserved must be 0");
   if (c->table_stride < c->pages_per_seq && c->batch > 1) return fail_inval("table_stride is less than pages_per_seq");
@@ -214,6 +215,7 @@ int paged_attn_layout(const shadowkv_paged_cache* c, int hq, int n_tokens, Paged
   L->G = hq / c->n_kv_heads;
   if (L->G > 64) return fail_inval("group size above 64 is not supported");
   if (n_tokens < 0) return fail_inval("n_tokens must be >= 0");
+  if (n_tokens > kMaxSeqTokens) return fail_inval("more than 2^30 tokens");   // (block counts are 32 bits wide)
   L->block_rows = paged_attn_block_rows(L->G, ((long)n_tokens + c->batch - 1) / c->batch * L->G);
   L->tb = L->block_rows / L->G;
   L->n_wg = paged_attn_workgroups(L->block_rows);

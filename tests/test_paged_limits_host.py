@@ -38,3 +38,12 @@ def test_arrays_that_span_more_than_there_is():
     for big in (dict(token_stride=1 << 47), dict(head_stride=1 << 46), dict(n_seqs=1 << 12, seq_stride=1 << 40, n_tokens=1)):
         assert rotate(rope(), heads(**big), heads(data=2 * FAKE)) == S.EINVAL and "span" in S.last_error(), S.last_error()
         assert rotate(rope(), heads(data=2 * FAKE), heads(**big)) == S.EINVAL and "span" in S.last_error()
+
+
+def test_more_new_tokens_than_a_cache_has_room_for():
+    """2^30 is what a sequence holds; beyond it, rows of blocks leave 32 bits."""
+    many = dict(n_tokens=(1 << 31) - 1)
+    assert attend(cache(batch=1), q=heads(**many), out=heads(data=1 << 45, **many), ws=None) == S.EINVAL and "2^30" in S.last_error()
+    most = dict(n_tokens=1 << 30)
+    assert attend(cache(batch=1), q=heads(**most), out=heads(data=1 << 45, **most), ws=None) == S.EWORKSPACE
+    assert S.lib().shadowkv_paged_attention_workspace_bytes(C.byref(cache(batch=1)), 4, (1 << 31) - 1) == 0
