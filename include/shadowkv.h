@@ -407,7 +407,7 @@ typedef struct shadowkv_paged_cache {
  *   rope       NULL: keys are stored as they come; q and q_out must be NULL then
  *   k, v       [1, T, h_kv, d]  bf16, or the cache's type; both the same
  *   q, q_out   [1, T, h_q, d]   bf16 both, or both NULL; q_out may be q itself
- *   seq_starts dev [batch + 1] int32, ascending; NULL: T / batch tokens of every sequence (batch must divide T)
+ *   seq_starts dev [batch + 1] int32, ascending, held to [0, T]; NULL: T / batch tokens of every sequence (batch must divide T)
  *   kv_lens    dev [batch] int32
  *   pos_offset dev [batch] int32 or NULL (0)
  * No place may be written twice in a call.  T <= 2^27.

@@ -203,7 +203,7 @@ __global__ __launch_bounds__(kRopeNT) void append_paged_kernel(RopeArgs rope, in
     }
     seq = lo - 1;
     if (seq < 0 || seq >= runs.batch) return;   // outside every run
-    end = in_lds ? starts[seq + 1] : g[seq + 1];
+    end = min(in_lds ? starts[seq + 1] : g[seq + 1], runs.n_tokens);   // (held to the rows there are, as attention holds it)
   }
   const int64_t place = (int64_t)runs.kv_lens[seq] - ((int64_t)end - tok);
   const int blocks = (hkv + kHeadsPerBlock - 1) / kHeadsPerBlock, y = blockIdx.y;

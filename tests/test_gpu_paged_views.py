@@ -42,3 +42,19 @@ def test_heads_of_one_projection_beside_each_other():
     assert torch.equal(both[:, 1::2], S.paged_attention(c, want, lens)) and torch.equal(both[:, ::2], want)
     with pytest.raises(S.ShadowKVError, match="share memory"):
         S.paged_append(c, k[:-1], v[:-1], lens, rope=r, q=q[:-1], q_out=q[1:])
+
+
+def test_starts_that_reach_beyond_the_rows():
+    """Held to the rows there are, for appending as for attention: the last row goes to the last place."""
+    t, hkv, hq, d = 9, 2, 4, 64
+    cache = Cache([20, 33], hkv, d, BF, 16, seed=3)
+    k, v, q = _x(1, t, hkv, d), _x(2, t, hkv, d), _x(3, t, hq, d)
+    r, lens = S.Rope(d), cache.kv_lens()
+    got = []
+    for starts in ([0, 4, t], [-3, 4, t + 5]):
+        c = S.PagedCache(cache.k.clone(), cache.v.clone(), cache.table)
+        starts = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        qq = S.paged_append(c, k, v, lens, seq_starts=starts, rope=r, q=q)
+        got.append((c.k.view(torch.int16), c.v.view(torch.int16), qq, S.paged_attention(c, qq, lens, seq_starts=starts)))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
