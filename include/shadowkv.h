@@ -356,7 +356,8 @@ typedef struct shadowkv_rope {
 } shadowkv_rope;
 
 /* The rot_dim/2 frequencies in radians per position, to host memory (fp64).  Rounded to fp32 on the device they are the
- * inv_freq of shadowkv_params.  Returns SHADOWKV_OK or SHADOWKV_EINVAL (also where rope->inv_freq is set). */
+ * inv_freq of shadowkv_params; that rounding turns a pair by up to 2^-25 of its position in radians (0.03 at 1M tokens), so
+ * what a decode step with them is to read is rotated with the same fp32 numbers as inv_freq here.  Returns SHADOWKV_OK or SHADOWKV_EINVAL (also where rope->inv_freq is set). */
 int shadowkv_rope_frequencies(const shadowkv_rope *rope, double *out);
 
 /*

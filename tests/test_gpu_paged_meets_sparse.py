@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2410_21465_amd import shadowkv as S
-from paged_util import BF, attention, pair_size, turned
+from paged_util import BF, attention, check_turned, pair_size, turned
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +67,34 @@ def test_a_decode_step_over_an_appended_prompt_attends_over_its_keys():
         off = (turned(rope, raw, pos) - k_rope[i].transpose(0, 1)).norm()
         assert off <= 1.1 * tail + 2.0 ** -7 * size.norm() + 2.0 ** -8 * k_rope[i].norm()
         assert off < 0.1 * (raw - k_rope[i].transpose(0, 1)).norm()
+
+
+@pytest.mark.parametrize("at", [0, 131072, 1048576 - 512])
+def test_rotations_far_along_agree_where_both_get_the_same_frequencies(at):
+    """A decode step takes its frequencies in fp32.  Keys that it rebuilds are those that `rotate` makes with the same fp32 numbers as its
+    inv_freq, wherever they stand; with the unrounded ones they are up to 2^-25 of the position in radians apart."""
+    b, hkv, d, s, r = 1, 2, 64, 512, 64
+    scaled = S.Rope(d, scaling=S.ROPE_BANDS, factor=8.0, low=1.0, high=4.0, original_len=8192)
+    inv = scaled.frequencies().float().cuda()
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    rows = torch.randn(hkv, r, d, generator=gen, device="cuda").to(BF)
+    A = torch.eye(r, device="cuda").repeat(s // r, 1)[None].to(BF).contiguous()                     # token t is row t % r of B, exactly
+    keys = rows.transpose(0, 1).repeat(s // r, 1, 1)                                                # [s, hkv, d]
+    p = S.Params(b, 4, hkv, d, s, chunk_size=8, rank=r, n_outlier_chunks=0, topk_chunks=s // 8, local_len=0, inv_freq=inv,
+                 flags=S.FLAG_KEEP_REBUILT_KEYS)
+    off = torch.tensor([at], dtype=torch.int32, device="cuda")
+    k_rope = S.rotate(S.Rope(d, inv_freq=inv), keys[None], pos_offset=off)
+    store = torch.randn(b, hkv, s, d, generator=gen, device="cuda").to(BF)
+    pre = S.build_landmarks(p, k_rope.transpose(1, 2).contiguous(), store)
+    _, ids, ws = S.decode_step(p, _q(b, 4, d, 9), A, rows[None].contiguous(), pre["landmarks"], pre["landmark_chunk_ids"], pre["k_outlier"],
+                               pre["v_outlier"], None, None, store, off)
+    assert torch.equal(ids[0], torch.arange(s // 8, dtype=torch.int32, device="cuda").expand(hkv, -1))
+    rebuilt = S.workspace_view(p, ws, "k_sparse")[0].transpose(0, 1).double()                       # [s, hkv, d], fp32
+    pos = at + torch.arange(s, device="cuda")
+    check_turned(S.Rope(d), k_rope[0], keys, pos, freq=inv.double().cpu())
+    size = pair_size(S.Rope(d), keys.double())
+    assert ((rebuilt - k_rope[0].double()).abs() <= 2.0 ** -8 * rebuilt.abs() + 2.0 ** -18 * size).all()
+    apart = (turned(S.Rope(d), keys.double(), pos, freq=scaled.frequencies()) - rebuilt).abs() / size
+    assert (apart <= 2.0 ** -25 * (at + s) + 2.0 ** -18).all()
+    if at > 1000000:
+        assert apart.max() > 2.0 ** -8                                                              # more than a rounding to bf16
