@@ -62,7 +62,8 @@ __device__ __forceinline__ uint32_t e5m2x2_to_bf16x2(uint32_t w) {
   return (__float_as_uint(f[0]) >> 16) | (__float_as_uint(f[1]) & 0xffff0000u);
 }
 
-// two fp32 as two bf16, nearest even, and four as four E5M2 (v_cvt_pk_bf8_f32: f32_to_e5m2's result for every fp32 pattern)
+// two fp32 as two bf16, nearest even, and four as four E5M2 (v_cvt_pk_bf8_f32 rounds to nearest even, to infinity where that leaves the range, and keeps
+// subnormals and NaN: compared for all 2^32 inputs with the integer form of f64_to_e5m2)
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
   const f32x2_t x = {lo, hi};
@@ -76,8 +77,8 @@ __device__ __forceinline__ uint32_t pack_e5m2(float a, float b, float c, float d
 // the result is infinity, as in IEEE 754): fp64 -> fp32 by round-to-odd, then
 // the fp32 is rounded at its 21st fraction bit, in integer arithmetic so that a carry moves into the
 // exponent by itself; below 2^-14 the codes are equally spaced (2^-16).
-__device__ __forceinline__ uint8_t f32_to_e5m2(float x) {
-  const uint32_t u = __float_as_uint(x);
+__device__ __forceinline__ uint8_t f64_to_e5m2(double x) {
+  const uint32_t u = __float_as_uint(f64_to_f32_odd(x));
   const uint32_t sign = (u >> 24) & 0x80u, a = u & 0x7fffffffu;
   // |f| >= 2^-14: 8 exponent bits | 2 fraction bits, rebiased, infinity beyond; else 0..4 (4 is the smallest normal)
   const uint32_t big = min(((a + 0xfffffu + ((a >> 21) & 1u)) >> 21) - (uint32_t)((127 - 15) << 2), 0x7cu);
@@ -85,7 +86,6 @@ __device__ __forceinline__ uint8_t f32_to_e5m2(float x) {
   const uint32_t code = a >= 0x38800000u ? big : tiny;
   return (uint8_t)(sign | (a > 0x7f800000u ? 0x7fu : code));
 }
-__device__ __forceinline__ uint8_t f64_to_e5m2(double x) { return f32_to_e5m2(f64_to_f32_odd(x)); }
 
 // ---- order-preserving key of a double (larger value <=> larger key, never 0 for
 // finite or infinite inputs).  -0.0 is folded onto +0.0 first.

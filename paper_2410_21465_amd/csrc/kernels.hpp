@@ -255,7 +255,7 @@ struct PagedAttnArgs {
 // Rows (tokens x query heads per KV head) of a row block: 16 or 32 where a workgroup's waves share out the keys, 128 where
 // they share out the rows.  rows: what a sequence has on average.
 int paged_attn_block_rows(int G, long rows);
-int paged_attn_workgroups(int block_rows);
+int paged_attn_workgroups();
 hipError_t launch_paged_attention(PagedAttnArgs a, int block_rows, hipStream_t st);
 
 }  // namespace skv

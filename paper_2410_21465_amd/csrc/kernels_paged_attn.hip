@@ -141,7 +141,7 @@ __global__ __launch_bounds__(NT) void paged_attn_join_kernel(PagedAttnArgs a, in
 
 // (up to 32 rows the kernel that reads keys fastest and weighs in two terms, else the one with the most products per byte read)
 int paged_attn_block_rows(int G, long rows) { return G <= 16 && rows <= 16 ? 16 : G <= 32 && rows <= 32 ? 32 : kTileRows; }
-int paged_attn_workgroups(int block_rows) { return kMaxWg; }   // two per compute unit; a multiple of eight
+int paged_attn_workgroups() { return kMaxWg; }   // two per compute unit; a multiple of eight
 
 hipError_t launch_paged_attention(PagedAttnArgs a, int block_rows, hipStream_t st) {
   hipError_t e = a.kv_bytes == 1 ? launch_paged_attn_fp8(a, block_rows, st) : launch_paged_attn_eb<2>(a, block_rows, st);

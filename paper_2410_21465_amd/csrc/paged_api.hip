@@ -218,7 +218,7 @@ int paged_attn_layout(const shadowkv_paged_cache* c, int hq, int n_tokens, Paged
   if (n_tokens > kMaxSeqTokens) return fail_inval("more than 2^30 tokens");   // (block counts are 32 bits wide)
   L->block_rows = paged_attn_block_rows(L->G, ((long)n_tokens + c->batch - 1) / c->batch * L->G);
   L->tb = L->block_rows / L->G;
-  L->n_wg = paged_attn_workgroups(L->block_rows);
+  L->n_wg = paged_attn_workgroups();
   const size_t rows = (size_t)2 * L->n_wg * L->block_rows;
   size_t off = 0;
   L->desc = off; off += up((size_t)L->n_wg * sizeof(int4));
