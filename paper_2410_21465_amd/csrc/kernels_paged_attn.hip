@@ -32,7 +32,7 @@ struct Joined {   // a row's state as parts are added
 // rows, 5 us behind a prompt of 8K tokens; 3 us of that go into finding the parts.  256 threads for up to 32 rows (with 512 the first
 // two took 6 and 13, with 128 the 256 parts of a token over 1M keys 22 instead of 15), 512 for 128 rows (1024: 34 us against 28 for 32 tokens
 // over 16.7K keys on 14/2 heads, the whole call).
-constexpr int kFewParts = 16, kMaxWg = 512;
+constexpr int kMaxWg = 512;
 template <int NT>
 __global__ __launch_bounds__(NT) void paged_attn_join_kernel(PagedAttnArgs a, int block_rows) {
   static_assert(kMaxWg % NT == 0);
@@ -94,8 +94,10 @@ __global__ __launch_bounds__(NT) void paged_attn_join_kernel(PagedAttnArgs a, in
     if (c < a.d) j.finish(a, (int64_t)it.desc.y + tl, it.desc.z * a.G + row - tl * a.G, c);
   };
   const Item own = item_of(0), around = item_of(1);
-  // (one way takes a trip to memory per eight parts, the other one per row of a workgroup, of which it has rows / parts)
-  auto few = [&](const Item& it) { return it.parts <= kFewParts || it.parts * it.parts <= 12 * it.desc.w; };
+  // One way takes a trip to memory per eight parts, the other one per row of a workgroup, of which it has rows / parts: the border
+  // lies where parts^2 is some multiple of the rows.  Whole calls, at 3 / 12 / 48 times: 32 tokens over 8K and 30K keys on 32/4 heads 44.5 / 38.0 /
+  // 38.0 and 69.6 / 63.2 / 63.3 us, over 16K on 32/8 heads 38.1 / 38.1 / 43.5, ten tokens over 3K on 32/2 heads 23.5 / 23.5 / 26.4.
+  auto few = [&](const Item& it) { return it.parts * it.parts <= 12 * it.desc.w; };
   auto join_few = [&](const Item& it, bool is_own) {
     if (it.parts == 0 || !few(it)) return;
     const bool alone = it.desc.w <= kHalf;   // (joined where it began, whose descriptor is at hand)
