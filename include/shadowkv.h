@@ -433,8 +433,9 @@ int shadowkv_paged_append(const shadowkv_paged_cache *cache, const shadowkv_rope
  *   workspace  dev >= shadowkv_paged_attention_workspace_bytes(), 256-byte aligned; its contents do not matter.  Two
  *              calls whose work may overlap need a workspace each.
  * Products and sums are fp32; the softmax weights are rounded to bf16 for the product with the values where a call has more than
- * 32 rows (tokens x h_q / h_kv) a sequence on average, and enter as two bf16 terms otherwise.  Results do not depend on what else runs:
- * the same call gives the same bits.
+ * 32 rows (T x h_q / h_kv, divided by batch) a sequence on average, and enter as two bf16 terms otherwise.  So a token's weights may
+ * enter with 8 bits or with 16 according to what else is in its call, rows outside every run included: off by up to 2^-8 of sum |weight value|, or 2^-16.
+ * The same call gives the same bits, whatever else the GPU does.
  */
 int shadowkv_paged_attention(const shadowkv_paged_cache *cache, const shadowkv_heads *q, const shadowkv_heads *out,
                              float *lse, const int32_t *seq_starts, const int32_t *kv_lens, int32_t causal,

@@ -345,7 +345,10 @@ int shadowkv_paged_attention(const shadowkv_paged_cache* cache, const shadowkv_h
   a.scale_log2 = scale_log2;
   a.tb = L.tb;
   a.n_wg = L.n_wg;
-  a.min_share = 128;   // (with 512, six tokens over 4K keys take 34 us instead of 29; with 256, 17 tokens over 600 keys 25 instead of 22)
+  // 64 / 128 / 256 / 512 keys, us: a token over 4K keys 19.6 / 18.3 / 19.4 / 22.4, eight sequences of 1K (14/2 heads of 64, 3 tokens) 19.1 / 16.7 /
+  // 17.7 / 21.4; with blocks of 128 rows 17 tokens over 600 keys of four sequences 25.9 / 22.5 / 26.2 / 32.0, 64 over 4K 35.0 / 35.0 / 32.6 / 35.8, 512 over
+  // 512 32.0 / 33.9 / 31.7 / 37.6; no difference from 256 tokens over 4K keys on
+  a.min_share = 128;
   a.desc = reinterpret_cast<int4*>(ws + L.desc);
   a.part_acc = reinterpret_cast<float*>(ws + L.part_acc);
   a.part_ml = reinterpret_cast<float2*>(ws + L.part_ml);

@@ -187,7 +187,8 @@ __device__ __forceinline__ Share get_share(const PagedAttnArgs& a, int64_t* foun
 }
 
 // The workgroup's items one after the other: work(run, seq, head, blk, first tile, last tile + 1, part slot or -1).  What is only wanted
-// between items waits in LDS (a copy per wave): in scalar registers it made the loops over keys spill theirs.
+// between items waits in LDS (a copy per wave): in scalar registers it made the loops over keys spill theirs.  Ten to 63 scalar registers
+// are still put into lanes of vector registers, outside those loops but for two to five reads a tile in the branch for masked ones.
 template <int TILE, class F>
 __device__ __forceinline__ void for_items(const PagedAttnArgs& a, F&& work) {
   struct State {
@@ -332,6 +333,10 @@ __device__ __forceinline__ uint64_t row_offset(uint32_t units, int src) {   // b
 // 28K 1.04 ms = 0.94 PFLOP/s (a bf16 product of 8192^3 reaches 1.3; zeros in place of random data run a third faster there and a
 // quarter here: both are held by power).  Slower: the next tile's first half multiplied behind the weights (710 against 687 us),
 // 64 rows a wave and one wave per SIMD (0.5 to 0.7 of the rate), the maximum settled per 32 keys (643 against 621 us).
+// The weights are rounded to bf16 for P V, since a second term as for few rows would make half as many products again of what bounds the
+// kernel; the sum l takes them unrounded.  Each is off by 2^-8 of itself at most, either way, so the errors of a row's many keys
+// cancel for the most part: against 64 bits the outputs of a prompt and of chunks are off by 0.0022 of their size (root mean square), where
+// their own rounding to bf16 alone makes 0.0017.
 constexpr int kTileKeys = 64, kTileRows = 128, kTileNT = 256;
 template <int D>
 struct TilePitch {
@@ -673,7 +678,8 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
   constexpr int kVBytes = NW * kRowsKeys * PV, kMergeBytes = NW * BR * (D * 4 + 8);
   __shared__ __attribute__((aligned(16))) uint8_t lds[kVBytes > kMergeBytes ? kVBytes : kMergeBytes];
   // Q of two row blocks of long heads waits in LDS, in operand order: in registers, heads of 128 spilled 54 of theirs (259 us
-  // against 234, 16 sequences of 16K keys, 8 tokens each, 32 heads on 8), while heads of 64 have room for it (41.4 us against 42.4)
+  // against 234, 16 sequences of 16K keys, 8 tokens each, 32 heads on 8), while heads of 64 have room for it (41.4 us against 42.4).
+  // bf16 heads of 128 still spill 26, to scratch and back outside the loop over keys.
   constexpr bool kQInLds = NB == 2 && D > 64;
   __shared__ uint4 q_lds[kQInLds ? NB * kSteps : 1][kWave];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, col = lane & 15, quarter = lane >> 4;
