@@ -330,8 +330,9 @@ __device__ __forceinline__ uint64_t row_offset(uint32_t units, int src) {   // b
 //
 // Bound by the matrix pipe and the softmax's vector instructions, each busy for 44 % of a prompt's cycles: with two waves per SIMD
 // (256 registers a wave) they overlap only in part.  32/8 heads of 128: a prompt of 8K tokens 605 us = 0.91 PFLOP/s, 2K tokens after
-// 28K 1.04 ms = 0.94 PFLOP/s (a bf16 product of 8192^3 reaches 1.3; zeros in place of random data run a third faster there and a
-// quarter here: both are held by power).  Slower: the next tile's first half multiplied behind the weights (710 against 687 us),
+// 28K 1.04 ms = 0.94 PFLOP/s, on other cards up to 693 us and 1.19 ms (a bf16 product of 8192^3 reaches 1.3; zeros in place of random
+// data run a third faster there and a quarter here: both are held by power).  Slower: the next tile's first half multiplied behind the
+// weights (710 against 687 us),
 // 64 rows a wave and one wave per SIMD (0.5 to 0.7 of the rate), the maximum settled per 32 keys (643 against 621 us).
 // The weights are rounded to bf16 for P V, since a second term as for few rows would make half as many products again of what bounds the
 // kernel; the sum l takes them unrounded.  Each is off by 2^-8 of itself at most, either way, so the errors of a row's many keys
