@@ -7,6 +7,7 @@
 // only where the softmax with its maximum taken out would too.  (With m at the maximum, and weights of up to 2^8 let through before it
 // moves, which is the same arithmetic 2^8 higher up, finite values from 2^120 on came out infinite.)  The largest weight lies in
 // [2^-8, 1]; weights and sums are fp32, whose exponents have room for that at the lower end: bf16's smallest values come out exact.
+// A row's m follows its own logits alone, so that no bit of its result depends on the rows beside it and on keys that only they see.
 //
 // Both kernels form S^T = K Q^T, so that a lane of the matrix instruction's result holds one row's logits: the maximum
 // and the sum stay in the lane but for one exchange, the factors of a row are scalars of its lane, and P^T is already laid out as
@@ -543,7 +544,7 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
       read_values(0, vf[0]);   // arrives while the weights are formed
       top = max_halves(top) * a.scale_log2;
       if (__any(top > m)) {
-        const float next_m = fmaxf(m, top + kHeadroom), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next_m);
+        const float next_m = top > m ? top + kHeadroom : m, f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next_m);
         m = next_m;
         l *= f;
 #pragma unroll
@@ -841,7 +842,7 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
         for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
         top = max_quarters(top);
         if (__any(top > m[n])) {
-          const float next = fmaxf(m[n], top + kHeadroom), f = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - next);
+          const float next = top > m[n] ? top + kHeadroom : m[n], f = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - next);
           m[n] = next;
           l[n] *= f;
 #pragma unroll
