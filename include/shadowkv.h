@@ -420,8 +420,8 @@ int shadowkv_paged_append(const shadowkv_paged_cache *cache, const shadowkv_rope
 /*
  * Attention of new tokens over the paged cache, which holds them already: for token j of the n_i of sequence i and query head g,
  *   out = sum over the places l it sees of softmax_l(scale <q, k_l>) v_l   (KV head g / (h_q / h_kv)),
- * where it sees l <= kv_lens[i] - n_i + j with causal != 0, else every l < kv_lens[i].  kv_lens is held to
- * [0, pages_per_seq * page_size].  What a token does not see (later tokens, entries without a page, rows behind the
+ * where it sees l <= kv_lens[i] - n_i + j with causal != 0, else every l < kv_lens[i]; places below 0 or beyond
+ * pages_per_seq pages, which shadowkv_paged_append drops, hold nothing.  A negative kv_lens counts as 0.  What a token does not see (later tokens, entries without a page, rows behind the
  * length) has no influence on it, whatever is stored there, NaN and infinities among it.  A token that sees nothing, or whose logits
  * are all minus infinity, gets out = 0 and lse = -inf.  An infinite value that a token does see makes its element infinite; NaN where
  * infinities of both signs meet, and possibly where its weight is less than 2^-90 of the largest.

@@ -36,6 +36,7 @@ constexpr int kPartTail = 1, kPartHead = 2, kPartLast = 4;   // flags of a workg
 // ---- sharing out ----------------------------------------------------------------------------------------------------
 struct SeqRun {
   int start, n, len;   // first row, new tokens, tokens in the cache
+  int first;           // place of the first new token (below 0 or beyond len where the cache does not hold it)
 };
 __device__ __forceinline__ SeqRun get_run(const RunsArg& r, const PageTableArg& pt, int i) {
   SeqRun s;
@@ -47,7 +48,9 @@ __device__ __forceinline__ SeqRun get_run(const RunsArg& r, const PageTableArg& 
     s.n = r.n_tokens / r.batch;
     s.start = i * s.n;
   }
-  s.len = (int)min((int64_t)max(r.kv_lens[i], 0), (int64_t)pt.per_seq << pt.shift);
+  const int len = max(r.kv_lens[i], 0);
+  s.len = (int)min((int64_t)len, (int64_t)pt.per_seq << pt.shift);
+  s.first = len - s.n;
   return s;
 }
 // Work of one head of a sequence, in keys.  Block m's is base + slope (m + 1); the blocks are taken from both ends in turn (last,
@@ -64,7 +67,7 @@ struct SeqCost {
 __device__ __forceinline__ SeqCost get_cost(const SeqRun& s, int tb, int causal) {
   SeqCost c;
   c.blocks = (s.n + tb - 1) / tb;
-  c.base = kItemKeys + (causal ? max(s.len - s.n, 0) : s.len);
+  c.base = kItemKeys + (causal ? min(max(s.first, 0), s.len) : s.len);
   c.slope = causal ? tb : 0;
   return c;
 }
@@ -220,7 +223,7 @@ __device__ __forceinline__ void for_items(const PagedAttnArgs& a, F&& work) {
     const SeqCost c = get_cost(run, a.tb, a.causal);
     const int64_t cost = c.cost(p);
     const int blk = c.block(p);
-    const int seen = a.causal ? min(max(run.len - run.n + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
+    const int seen = a.causal ? min(max(run.first + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
     const int tiles = (seen + TILE - 1) / TILE;
     auto tile_at = [&](int64_t x) {
       return x >= cost ? tiles : x <= kItemKeys ? 0 : (int)min((int64_t)tiles, (x - kItemKeys) / TILE);
@@ -361,9 +364,9 @@ __global__ __launch_bounds__(kTileNT, 2) void paged_attn_tiles_kernel(PagedAttnA
   for_items<kTileKeys>(a, [&](const SeqRun& run, int seq, int head, int blk, int t0, int t1, int slot) {
     const int G = a.G, row = wave * 32 + col, tl = row / G, g = row - tl * G, tok = blk * a.tb + tl;
     const bool row_ok = tl < a.tb && tok < run.n;
-    const int limit = row_ok ? (a.causal ? run.len - run.n + tok : run.len - 1) : -1;   // last key the row sees
+    const int limit = row_ok ? (a.causal ? run.first + tok : run.len - 1) : -1;   // last key the row sees
     // tiles before `clear` are seen whole by every row of the block
-    const int first = a.causal ? run.len - run.n + blk * a.tb : run.len - 1, clear = max(first + 1, 0) / kTileKeys;
+    const int first = a.causal ? run.first + blk * a.tb : run.len - 1, clear = max(first + 1, 0) / kTileKeys;
     const int64_t qrow = run.start + tok;
     bf16x8 qf[QS];
     {
@@ -695,7 +698,7 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
       return 64 * (s / 2) + 16 * quarter + 8 * (s % 2);
     };
     const int32_t* table = a.pt.table + seq * a.pt.stride;
-    const int seen = a.causal ? min(max(run.len - run.n + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
+    const int seen = a.causal ? min(max(run.first + min(run.n, (blk + 1) * a.tb), 0), run.len) : run.len;
     const int s0 = t0 * NW + wave, last = min(t1 * NW, (seen + kRowsKeys - 1) / kRowsKeys);   // in tiles of 32 keys
     auto lookup = [&](int t) { return page_entry(a, table, t * kRowsKeys + (lane & 31), run.len); };
     const int page0 = lookup(s0);
@@ -706,7 +709,7 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
     for (int n = 0; n < NB; ++n) {
       const int row = 16 * n + col, tl = row / G, g = row - tl * G, tok = blk * a.tb + tl;
       const bool ok = tl < a.tb && tok < run.n;
-      limit[n] = ok ? (a.causal ? run.len - run.n + tok : run.len - 1) : -1;
+      limit[n] = ok ? (a.causal ? run.first + tok : run.len - 1) : -1;
       // (rows that are none take row 0 of q: what they make is not written)
       const uint8_t* qp = a.q.p + (ok ? (run.start + tok) * a.q.tok + (head * G + g) * a.q.head : 0);
 #pragma unroll
@@ -719,7 +722,7 @@ __global__ __launch_bounds__(kRowsNT, 2) void paged_attn_rows_kernel(PagedAttnAr
       }
     }
     if constexpr (kQInLds) __syncthreads();
-    const int first = a.causal ? run.len - run.n + blk * a.tb : run.len - 1, clear = max(first + 1, 0) / kRowsKeys;
+    const int first = a.causal ? run.first + blk * a.tb : run.len - 1, clear = max(first + 1, 0) / kRowsKeys;
     f32x4 o[NB][DB];
     float m[NB], l[NB];
 #pragma unroll

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2410_21465_amd import shadowkv as S
-from paged_util import BF, F8, Cache
+from paged_util import BF, F8, Cache, attention
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +41,26 @@ def test_a_token_does_not_depend_on_the_queries_beside_it(n, hq):
         other = (q.float() * 20).to(BF)
         other[keep] = q[keep]
         assert torch.equal(S.paged_attention(cache.c, other, cache.kv_lens())[keep], was[keep])
+
+
+@pytest.mark.parametrize("n,over", [(10, 6), (10, 10), (10, 300), (60, 23), (3, 1)])
+def test_runs_that_reach_beyond_the_pages(n, over):
+    """A length that its pages do not hold: what paged_append drops is not there, and the tokens that it stored see what lies up to
+    their places, as without the ones that were dropped."""
+    d, hkv, hq, page, width = 64, 2, 8, 16, 5
+    cache = Cache([page * width, 40], hkv, d, BF, page, seed=9, width=width)
+    cap = page * width
+    lens, starts = torch.tensor([cap + over, 40], dtype=torch.int32, device="cuda"), cache.starts([n, 1])
+    k, v, q = (torch.randn(n + 1, h, d, generator=torch.Generator(device="cuda").manual_seed(h), device="cuda").to(BF) for h in (hkv, hkv, hq))
+    S.paged_append(cache.c, k, v, lens, seq_starts=starts)
+    lse = torch.empty(n + 1, hq, device="cuda")
+    out = S.paged_attention(cache.c, q, lens, seq_starts=starts, lse=lse)
+    pg = cache.table[0, torch.arange(cap, device="cuda") // page].long()
+    rows = torch.arange(cap, device="cuda") % page
+    kd, vd = cache.k[pg, :, rows].double(), cache.v[pg, :, rows].double()
+    limit = torch.arange(cap + over - n, cap + over, device="cuda").clamp(max=cap - 1)
+    want, want_lse, av, size = attention(q[:n].double(), kd, vd, limit, d ** -0.5)
+    delta = 2 * (d + 16) * 2.0 ** -24 * size + 2.0 ** -20
+    tol = 2.0 ** -8 * want.abs() + (1 + 2.0 ** -8) * (2.0 ** -8 + delta[..., None]) * av
+    assert ((out[:n].double() - want).abs() <= tol).all()
+    assert ((lse[:n].double() - want_lse).abs() <= delta + 2.0 ** -22 * (want_lse.abs() + 1)).all()
