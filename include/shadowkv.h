@@ -357,7 +357,8 @@ typedef struct shadowkv_rope {
 
 /* The rot_dim/2 frequencies in radians per position, to host memory (fp64).  Rounded to fp32 on the device they are the
  * inv_freq of shadowkv_params; that rounding turns a pair by up to 2^-25 of its position in radians (0.03 at 1M tokens), so
- * what a decode step with them is to read is rotated with the same fp32 numbers as inv_freq here.  Returns SHADOWKV_OK or SHADOWKV_EINVAL (also where rope->inv_freq is set). */
+ * what a decode step with them is to read is rotated with the same fp32 numbers as inv_freq here.  Returns SHADOWKV_OK or
+ * SHADOWKV_EINVAL (also where rope->inv_freq is set). */
 int shadowkv_rope_frequencies(const shadowkv_rope *rope, double *out);
 
 /*
@@ -421,8 +422,8 @@ int shadowkv_paged_append(const shadowkv_paged_cache *cache, const shadowkv_rope
  * Attention of new tokens over the paged cache, which holds them already: for token j of the n_i of sequence i and query head g,
  *   out = sum over the places l it sees of softmax_l(scale <q, k_l>) v_l   (KV head g / (h_q / h_kv)),
  * where it sees l <= kv_lens[i] - n_i + j with causal != 0, else every l < kv_lens[i]; places below 0 or beyond
- * pages_per_seq pages, which shadowkv_paged_append drops, hold nothing.  A negative kv_lens counts as 0.  What a token does not see (later tokens, entries without a page, rows behind the
- * length) has no influence on it, whatever is stored there, NaN and infinities among it.  A token that sees nothing, or whose logits
+ * pages_per_seq pages, which shadowkv_paged_append drops, hold nothing.  A negative kv_lens counts as 0.
+ * What a token does not see (later tokens, entries without a page, rows behind the length) has no influence on it, whatever is stored there, NaN and infinities among it.  A token that sees nothing, or whose logits
  * are all minus infinity, gets out = 0 and lse = -inf.  An infinite value that a token does see makes its element infinite; NaN where
  * infinities of both signs meet, and possibly where its weight is less than 2^-90 of the largest.
  *
@@ -434,7 +435,8 @@ int shadowkv_paged_append(const shadowkv_paged_cache *cache, const shadowkv_rope
  *              calls whose work may overlap need a workspace each.
  * Products and sums are fp32; the softmax weights are rounded to bf16 for the product with the values where a call has more than
  * 32 rows (T x h_q / h_kv, divided by batch) a sequence on average, and enter as two bf16 terms otherwise.  So a token's weights may
- * enter with 8 bits or with 16 according to what else is in its call, rows outside every run included: off by up to 2^-8 of sum |weight value|, or 2^-16.
+ * enter with 8 bits or with 16 according to what else is in its call, rows outside every run included: off by up to 2^-8 of
+ * sum |weight value|, or 2^-16.
  * The same call gives the same bits, whatever else the GPU does.
  */
 int shadowkv_paged_attention(const shadowkv_paged_cache *cache, const shadowkv_heads *q, const shadowkv_heads *out,
