@@ -3,7 +3,8 @@
  *
  * Two main operations, both enqueue-only on caller-owned HIP streams (further down: the decode step
  * with a chunk cache of an offloaded value store, the append of generated tokens to the context, the
- * SVD line of the pre-filling algorithm, and the ArgTopK primitive on its own):
+ * SVD line of the pre-filling algorithm, and the ArgTopK primitive on its own; rotary positions, a paged
+ * cache and attention over it; the choice of a beam search, and the state that follows it):
  *
  *   shadowkv_build_landmarks  pre-filling algorithm (Alg. 1) after its SVD
  *                             line: chunk means of the post-RoPE keys,
@@ -444,6 +445,144 @@ int shadowkv_paged_attention(const shadowkv_paged_cache *cache, const shadowkv_h
                              double softmax_scale, void *workspace, size_t workspace_bytes, void *stream);
 /* For n_tokens = T rows and h_q = n_q_heads (0 if the arguments are invalid; pointers are not looked at). */
 size_t shadowkv_paged_attention_workspace_bytes(const shadowkv_paged_cache *cache, int32_t n_q_heads, int32_t n_tokens);
+
+/*
+ * ---- A search over several continuations: the choice over beams and vocabulary, and the state that follows it ----
+ *
+ * Rows are beams: group g (one prompt) has rows g * n_beams .. g * n_beams + n_beams - 1.  A step of a search chooses
+ * (shadowkv_beam_select), which names for every new row the row that it continues, its parent; then the state of the rows follows
+ * their parents: dense arrays in place (shadowkv_reorder_rows), sequences in pages (shadowkv_pages_update, shadowkv_pages_copy).
+ */
+#define SHADOWKV_LOGITS_BF16 0
+#define SHADOWKV_LOGITS_FP16 1
+#define SHADOWKV_LOGITS_FP32 2
+
+typedef struct shadowkv_logits {
+  const void *data;                      /* dev [n_groups, n_beams, vocab], aligned to its element */
+  int64_t group_stride, beam_stride;     /* elements, >= 0; the logits of a row are contiguous */
+  int32_t n_groups, n_beams, vocab;      /* n_groups >= 0, n_beams in [1, 64], vocab in [1, 2^30]; at most 2^20 rows */
+  int32_t dtype;                         /* SHADOWKV_LOGITS_* */
+} shadowkv_logits;
+
+/*
+ * The n_out best continuations of every group.  Row r offers every token v with a logit x_v above minus infinity:
+ *   score = scores[r] + c x_v - log sum_w exp(c x_w)   (c = logit_scale, the inverse of a temperature),
+ *   rank  = score / (lengths[r] + 1)^length_penalty,
+ * a finished row only itself: score = scores[r], rank = score / lengths[r]^length_penalty.  What a group chooses comes in descending
+ * order of rank; where ranks are equal the lower row goes first, and in a row the higher logit, then the lower token.
+ * A row offers nothing where its score is not finite, or (unless it is finished) where a logit is NaN or plus infinity or all are
+ * minus infinity.  Places that are left over get score -inf, parent -1, token -1, finished 0, length 0.
+ *
+ *   scores       dev [n_groups, n_beams] fp32: summed log-probabilities of the rows; -inf for rows that do not exist (all but one of a
+ *                group in the first step)
+ *   finished     dev [n_groups, n_beams] bytes, not 0: the row has ended; or NULL
+ *   lengths      dev [n_groups, n_beams] int32, tokens of a row (a rank divides by a length of at least 1); may be NULL with
+ *                length_penalty == 0
+ *   length_penalty in [-16, 16]; logit_scale 0 => 1, else positive and a normal number in fp32
+ *   end_token    in [-1, vocab): a row that takes it is finished; also the token that a finished row reports
+ *   n_out        in [1, 64]
+ *   out_scores   dev [n_groups, n_out] fp32, out_parents (rows 0 .. n_groups * n_beams - 1) and out_tokens int32;
+ *   out_finished (bytes, 0 or 1) and out_lengths (int32; those of the parent, + 1 unless it had finished; needs lengths) may be NULL.  With
+ *                n_out == n_beams they may be scores, finished and lengths themselves; no other arguments may share memory.
+ *   workspace    dev >= shadowkv_beam_select_workspace_bytes(), 256-byte aligned; its contents do not matter.  Two calls whose work
+ *                may overlap need a workspace each.
+ * Sums, logarithms and ranks are fp64, the sum of exponentials right to 2^-39 (so that scores of different rows nearer than 2^-37 are
+ * not told apart, unless the rows have the same logits); scores are rounded once.  The same call gives the same bits, and rows of equal
+ * logits equal sums, whatever their addresses are.
+ */
+int shadowkv_beam_select(const shadowkv_logits *logits, const float *scores, const uint8_t *finished, const int32_t *lengths,
+                         double length_penalty, double logit_scale, int32_t end_token, int32_t n_out, float *out_scores,
+                         int32_t *out_parents, int32_t *out_tokens, uint8_t *out_finished, int32_t *out_lengths,
+                         void *workspace, size_t workspace_bytes, void *stream);
+/* (0 if the sizes are invalid; pointers are not looked at) */
+size_t shadowkv_beam_select_workspace_bytes(const shadowkv_logits *logits, int32_t n_out);
+
+/* Rows of a dense state array: row i is n_outer pieces of `inner` bytes, at data + i * row_stride + j * outer_stride. */
+typedef struct shadowkv_rows {
+  void *data;                        /* dev */
+  int64_t row_stride, outer_stride;  /* bytes, >= 0 */
+  int64_t inner;                     /* bytes, >= 0 */
+  int32_t n_outer;                   /* >= 0 */
+  int32_t reserved;                  /* 0 */
+} shadowkv_rows;
+
+/*
+ * Replaces row i of every array by what row parents[i] was before the call, in place, in one launch for up to 64 arrays.  Rows with
+ * a parent outside [0, n_rows), and those that are their own parent, are left as they are (and not read).
+ *   arrays  host [n_arrays], n_arrays in [0, 4096]; an array may not overlap itself, another one of the call, or parents
+ *   parents dev [n_rows] int32, n_rows in [0, 2048]
+ * Pieces are moved 16 bytes at a time where the address, the strides and `inner` of an array are multiples of 16, else 4 or 1.
+ */
+int shadowkv_reorder_rows(const shadowkv_rows *arrays, int32_t n_arrays, const int32_t *parents, int32_t n_rows, void *stream);
+
+/*
+ * Who holds which page.  Sequence i of `batch` holds the first ceil(kv_lens[i] / page_size) entries of its row of the page table;
+ * page_refs[p] is the number of entries that hold page p, plus whatever the caller adds for holders of its own (a prefix kept
+ * for later); a page is free where it is 0.  Entries outside [0, n_pages) are no pages, and those behind a row's pages are written
+ * as -1.  The table is shared by the caches of all layers (shadowkv_paged_cache.page_table); an empty pool has kv_lens 0, page_refs 0.
+ */
+typedef struct shadowkv_page_pool {
+  int32_t *page_table;                             /* dev [batch, table_stride], the first pages_per_seq used */
+  int64_t table_stride;
+  int32_t *kv_lens;                                /* dev [batch], in [0, pages_per_seq * page_size] */
+  int32_t *page_refs;                              /* dev [n_pages] */
+  int32_t batch, pages_per_seq, n_pages;           /* batch in [1, 4096]; n_pages <= 2^28 */
+  int32_t page_size;                               /* a power of two, up to 65536 */
+} shadowkv_page_pool;
+
+/* Pages to be copied: move i takes the first rows[i] tokens (all with rows == NULL) of every head of page src[i] to page dst[i]. */
+typedef struct shadowkv_page_moves {
+  int32_t *src, *dst, *rows;                       /* dev [capacity] */
+  int32_t *count;                                  /* dev, moves that there are; NULL: capacity */
+  int32_t capacity;
+  int32_t reserved;                                /* 0 */
+} shadowkv_page_moves;
+
+/*
+ * Makes every sequence a continuation of another one, and room for its new tokens: row i becomes the first
+ *   kept_i = min(kv_lens[parents[i]], keep_lens[i])  tokens of what row parents[i] was before the call,
+ * and then, where that is granted, n_i further tokens that shadowkv_paged_append may write (kv_lens[i] = kept_i + n_i counts them,
+ * as it wants it).  Forking is two rows with one parent; a row whose parent lies outside [0, batch) is emptied (kept_i = 0);
+ * drafted tokens are taken back with keep_lens.
+ * Pages are shared and page_refs follow.  Where n_i > 0 and kept_i is no multiple of page_size the row's last page will be written:
+ * rows in ascending order, a row takes a copy of it unless it is the only holder left, so that the last of them keeps the page.  New
+ * pages and copies are the lowest free pages (after the pages that this call frees), in order of row and place.
+ * Granted are rows in ascending order until one needs more pages than are left: from there on, rows that need a page, or whose
+ * last page another one held, keep kept_i tokens and nothing more.  Rows with kept_i + n_i > pages_per_seq * page_size too, wherever they are.  A last page
+ * that is outside [0, n_pages) is not copied or replaced.
+ *
+ *   parents    dev [batch] int32 or NULL (every row itself);  keep_lens dev [batch] int32 or NULL (all; below 0 counts as 0)
+ *   n_new      dev [batch] int32 (below 0 counts as 0) or NULL: n_new_all (>= 0) of every row
+ *   moves      out: the copies to be made (rows: tokens that the page holds), before anything is appended; capacity >= batch, no
+ *              member NULL
+ *   workspace  dev >= shadowkv_pages_workspace_bytes(), 256-byte aligned, contents do not matter, one for each call that may overlap
+ * parents, keep_lens and n_new may not share memory with the pool.
+ */
+int shadowkv_pages_update(const shadowkv_page_pool *pool, const int32_t *parents, const int32_t *keep_lens, const int32_t *n_new,
+                          int32_t n_new_all, const shadowkv_page_moves *moves, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Moves pages in use down into free ones: the i-th free page from below takes what the i-th used page from above holds, as long
+ * as that lies above it and i < min(max_moves, moves->capacity).  page_refs follow, and the entries of the page table; other places where
+ * the caller holds page numbers are the caller's (moves->src, moves->dst).  Afterwards every page from *n_used on is free.
+ *   moves      out: the pages to be copied, in every layer; rows may be NULL (else page_size is written), the other members may not
+ *   n_used     dev out int32, or NULL
+ */
+int shadowkv_pages_compact(const shadowkv_page_pool *pool, int32_t max_moves, const shadowkv_page_moves *moves, int32_t *n_used,
+                           void *workspace, size_t workspace_bytes, void *stream);
+/* For shadowkv_pages_update and shadowkv_pages_compact (0 if the sizes are invalid; pointers are not looked at). */
+size_t shadowkv_pages_workspace_bytes(const shadowkv_page_pool *pool);
+
+/*
+ * Copies pages, keys and values, from cache to cache: from[l] to to[l] for every l < n_layers (to may be from: copies
+ * inside a cache).  from[l] and to[l] agree in n_kv_heads, head_dim, page_size and kv_dtype, and may differ in n_pages and strides; their page
+ * tables are not looked at and may be NULL.  Moves whose pages lie outside them are left out; rows[i] is held to [0, page_size].
+ * In a call no page may be written twice, or be read and written, and the pages of the layers may not overlap; a device cannot
+ * refuse that: such pages hold either contents, or parts of both.
+ *   from, to   host arrays of n_layers pointers;  n_layers in [0, 4096]
+ */
+int shadowkv_pages_copy(const shadowkv_paged_cache *const *from, const shadowkv_paged_cache *const *to, int32_t n_layers,
+                        const shadowkv_page_moves *moves, void *stream);
 
 /* Workspace sizes in bytes for the given shape (0 if params are invalid). */
 size_t shadowkv_build_workspace_bytes(const shadowkv_params *params);

@@ -258,4 +258,71 @@ int paged_attn_block_rows(int G, long rows);
 int paged_attn_workgroups();
 hipError_t launch_paged_attention(PagedAttnArgs a, int block_rows, hipStream_t st);
 
+// ---- a search over several continuations (kernels_beam.hip, kernels_reorder.hip, kernels_pages.hip) ----
+struct BeamPart {           // of a row: sum over a part of exp(c (x - ref)); bad: a logit is NaN or plus infinity
+  double sum;
+  float ref;                // -inf: no logit above minus infinity
+  int bad;
+};
+struct BeamArgs {
+  const uint8_t* logits;    // strides in bytes
+  int64_t group_stride, beam_stride;
+  int groups, beams, vocab, dtype, n;
+  int part_len, n_parts;    // tokens of a part (a multiple of 512), parts of a row
+  double scale, penalty;
+  const float* scores;
+  const uint8_t* finished;
+  const int32_t* lengths;
+  int end_token;
+  float* out_scores;
+  int32_t *out_parents, *out_tokens;
+  uint8_t* out_finished;
+  int32_t* out_lengths;
+  BeamPart* parts;          // [rows, n_parts]
+  uint2* best;              // [rows, n_parts, n] (logit as fp32 bits, token), descending; token ~0u: none
+};
+int beam_part_len(int64_t rows, int vocab);
+hipError_t launch_beam_select(const BeamArgs& a, hipStream_t st);
+
+constexpr int kMaxReorderRows = 2048, kMaxReorderArrays = 64;
+struct ReorderArray {
+  uint8_t* p;
+  int64_t row, outer;       // strides in bytes
+  int64_t units;            // of a piece
+  int32_t n_outer, unit;    // unit: 16, 4 or 1 bytes
+};
+struct ReorderArgs {
+  ReorderArray a[kMaxReorderArrays];
+  int n_arrays, n_rows;
+  const int32_t* parents;
+};
+hipError_t launch_reorder_rows(const ReorderArgs& a, hipStream_t st);
+
+constexpr int kMaxPoolRows = 4096;
+struct PoolArg {
+  int32_t* table;
+  int64_t stride;
+  int32_t *lens, *refs;
+  int batch, per_seq, n_pages, shift;   // shift: log2 of the page size
+};
+struct MovesArg {
+  int32_t *src, *dst, *rows;
+  int32_t* count;
+  int capacity;
+};
+// free_list: [n_pages]
+hipError_t launch_pages_update(const PoolArg& p, const int32_t* parents, const int32_t* keep, const int32_t* n_new, int n_new_all, const MovesArg& m,
+                               int32_t* free_list, hipStream_t st);
+// new_id: [n_pages], info: [4]
+hipError_t launch_pages_compact(const PoolArg& p, int max_moves, const MovesArg& m, int32_t* n_used, int32_t* new_id, int32_t* info, hipStream_t st);
+constexpr int kMaxCopyLayers = 32;
+struct PagesCopyArgs {      // layers of one geometry
+  const uint8_t *from_k[kMaxCopyLayers], *from_v[kMaxCopyLayers];
+  uint8_t *to_k[kMaxCopyLayers], *to_v[kMaxCopyLayers];
+  int64_t fk[3], fv[3], tk[3], tv[3];   // strides of page, head, token in bytes
+  int n_layers, hkv, row_bytes, page_size, from_pages, to_pages;
+  MovesArg m;
+};
+hipError_t launch_pages_copy(const PagesCopyArgs& a, hipStream_t st);
+
 }  // namespace skv

@@ -1,0 +1,97 @@
+// Rows of dense state arrays replaced in place by those of their parents: x[i] <- x_old[parents[i]], several arrays in a launch.
+//
+// A workgroup takes a slice of the bytes of all rows: it loads what the rows that change are to hold into registers, waits until all its
+// waves have theirs, and writes.  Slices have no bytes in common, so nothing else has to be ordered, whatever the parents are (cycles,
+// rows taken many times), and rows that stay cost nothing.  The fewer rows change, the wider the slice.
+#include "common.hpp"
+#include "kernels.hpp"
+
+namespace skv {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kHeld = 8;                                  // pieces of a thread
+constexpr int kSlots = kThreads * kHeld;                  // >= kMaxReorderRows: a slice is one unit wide at least
+static_assert(kSlots >= kMaxReorderRows, "a slice holds a unit of every row");
+
+template <class T>
+__device__ __forceinline__ void move_slice(const ReorderArray& a, const uint32_t* pairs, int n, int shift, int64_t first, int outer) {
+  T held[kHeld];
+  const int cols = 1 << shift;
+  uint8_t* base = a.p + outer * a.outer;
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const int item = k * kThreads + threadIdx.x, i = item >> shift;
+    const int64_t u = first + (item & (cols - 1));
+    if (i < n && u < a.units) held[k] = *reinterpret_cast<const T*>(base + (int64_t)(pairs[i] & 0xffffu) * a.row + u * (int64_t)sizeof(T));
+  }
+  __builtin_amdgcn_s_waitcnt(0);                          // what is loaded is there before any wave writes
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const int item = k * kThreads + threadIdx.x, i = item >> shift;
+    const int64_t u = first + (item & (cols - 1));
+    if (i < n && u < a.units) *reinterpret_cast<T*>(base + (int64_t)(pairs[i] >> 16) * a.row + u * (int64_t)sizeof(T)) = held[k];
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void reorder_rows_kernel(ReorderArgs g) {
+  __shared__ uint32_t pairs[kMaxReorderRows];             // (row << 16) | parent of the rows that change
+  __shared__ int64_t until[kMaxReorderArrays];            // slices of the arrays up to this one
+  __shared__ int n_shared, wave_sum[kThreads / kWave];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+  if (tid == 0) n_shared = 0;
+  __syncthreads();
+  for (int i0 = 0; i0 < g.n_rows; i0 += kThreads) {
+    const int i = i0 + tid;
+    const int p = i < g.n_rows ? g.parents[i] : -1;
+    const bool changes = p >= 0 && p < g.n_rows && p != i;
+    const uint64_t m = __ballot(changes);
+    if (lane == 0) wave_sum[wave] = __popcll(m);
+    __syncthreads();
+    int at = n_shared + __popcll(m & ((1ull << lane) - 1));
+    for (int v = 0; v < wave; ++v) at += wave_sum[v];
+    if (changes) pairs[at] = ((uint32_t)i << 16) | (uint32_t)p;
+    __syncthreads();
+    if (tid == kThreads - 1) n_shared = at + (changes ? 1 : 0);
+    __syncthreads();
+  }
+  const int n = n_shared;
+  if (n == 0) return;
+  const int shift = 31 - __clz(kSlots / n);               // 2^shift units wide: n << shift <= kSlots
+  if (tid == 0) {
+    int64_t sum = 0;
+    for (int k = 0; k < g.n_arrays; ++k) {
+      sum += (int64_t)g.a[k].n_outer * ((g.a[k].units + (1 << shift) - 1) >> shift);
+      until[k] = sum;
+    }
+  }
+  __syncthreads();
+  const int64_t total = until[g.n_arrays - 1];
+  int k = 0;
+  for (int64_t t = blockIdx.x; t < total; t += gridDim.x) {
+    while (t >= until[k]) ++k;
+    const ReorderArray a = g.a[k];
+    const int64_t per = (a.units + (1 << shift) - 1) >> shift, in = t - (k ? until[k - 1] : 0);
+    const int outer = (int)(in / per);
+    const int64_t first = (in % per) << shift;
+    if (a.unit == 16) move_slice<uint4>(a, pairs, n, shift, first, outer);
+    else if (a.unit == 4) move_slice<uint32_t>(a, pairs, n, shift, first, outer);
+    else move_slice<uint8_t>(a, pairs, n, shift, first, outer);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_reorder_rows(const ReorderArgs& a, hipStream_t st) {
+  // slices if all rows change; a workgroup takes several where there are more than fill the chip
+  int64_t slices = 0;
+  int shift = 0;
+  while ((a.n_rows << (shift + 1)) <= kSlots) ++shift;
+  for (int k = 0; k < a.n_arrays; ++k) slices += (int64_t)a.a[k].n_outer * ((a.a[k].units + (1 << shift) - 1) >> shift);
+  if (slices == 0) return hipSuccess;
+  reorder_rows_kernel<<<dim3((unsigned)(slices < 2048 ? slices : 2048)), kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace skv

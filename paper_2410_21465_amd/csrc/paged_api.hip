@@ -228,9 +228,128 @@ int paged_attn_layout(const shadowkv_paged_cache* c, int hq, int n_tokens, Paged
   return SHADOWKV_OK;
 }
 
+int check_pool(const shadowkv_page_pool* p, bool pointers) {
+  if (!p) return fail_inval("pool is NULL");
+  if (p->batch < 1 || p->batch > kMaxPoolRows) return fail_inval("batch must be in [1, %d]", kMaxPoolRows);
+  if (p->pages_per_seq < 1) return fail_inval("pages_per_seq must be >= 1");
+  if (p->n_pages < 1 || p->n_pages > (1 << 28)) return fail_inval("n_pages must be in [1, 2^28]");
+  if (p->page_size < 1 || p->page_size > 65536 || (p->page_size & (p->page_size - 1)))
+    return fail_inval("page_size must be a power of two in [1, 65536]");
+  if ((int64_t)p->pages_per_seq * p->page_size > kMaxSeqTokens) return fail_inval("more than 2^30 tokens a sequence");
+  if (p->batch > 1 && (p->table_stride < p->pages_per_seq || p->table_stride > ((int64_t)1 << 40)))
+    return fail_inval("table_stride must be in [pages_per_seq, 2^40]");
+  if (!pointers) return SHADOWKV_OK;
+  if (!p->page_table || !p->kv_lens || !p->page_refs) return fail_inval("page_table, kv_lens and page_refs must not be NULL");
+  return SHADOWKV_OK;
+}
+
+int check_moves(const shadowkv_page_moves* m) {
+  if (!m) return fail_inval("moves is NULL");
+  if (m->reserved) return fail_inval("reserved must be 0");
+  if (m->capacity < 0) return fail_inval("capacity must be >= 0");
+  return SHADOWKV_OK;
+}
+
+PoolArg pool_arg(const shadowkv_page_pool* p) {
+  int shift = 0;
+  while ((1 << shift) < p->page_size) ++shift;
+  return {p->page_table, p->table_stride, p->kv_lens, p->page_refs, p->batch, p->pages_per_seq, p->n_pages, shift};
+}
+MovesArg moves_arg(const shadowkv_page_moves* m) { return {m->src, m->dst, m->rows, m->count, m->capacity}; }
+
+size_t pages_workspace(const shadowkv_page_pool* p) { return kAlign + up((size_t)p->n_pages * sizeof(int32_t)); }
+
+// a cache whose pages alone matter
+int check_pages(const shadowkv_paged_cache* c, bool written) {
+  if (!c) return fail_inval("a cache is NULL");
+  shadowkv_paged_cache bare = *c;
+  bare.batch = bare.pages_per_seq = 1;
+  bare.page_table = static_cast<const int32_t*>(c->k);
+  return check_cache(&bare, true, written);
+}
+bool same_geometry(const shadowkv_paged_cache* a, const shadowkv_paged_cache* b) {
+  return a->k_page_stride == b->k_page_stride && a->k_head_stride == b->k_head_stride && a->k_token_stride == b->k_token_stride &&
+         a->v_page_stride == b->v_page_stride && a->v_head_stride == b->v_head_stride && a->v_token_stride == b->v_token_stride &&
+         a->n_pages == b->n_pages && a->n_kv_heads == b->n_kv_heads && a->head_dim == b->head_dim && a->page_size == b->page_size &&
+         a->kv_dtype == b->kv_dtype;
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t shadowkv_pages_workspace_bytes(const shadowkv_page_pool* pool) { return check_pool(pool, false) == SHADOWKV_OK ? pages_workspace(pool) : 0; }
+
+int shadowkv_pages_update(const shadowkv_page_pool* pool, const int32_t* parents, const int32_t* keep_lens, const int32_t* n_new, int32_t n_new_all,
+                          const shadowkv_page_moves* moves, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_pool(pool, true);
+  if (rc == SHADOWKV_OK) rc = check_moves(moves);
+  if (rc != SHADOWKV_OK) return rc;
+  if (!moves->src || !moves->dst || !moves->rows || !moves->count) return fail_inval("src, dst, rows and count of moves must not be NULL");
+  if (moves->capacity < pool->batch) return fail_inval("moves has room for %d, batch is %d", moves->capacity, pool->batch);
+  if (n_new_all < 0) return fail_inval("n_new_all must be >= 0");
+  rc = check_workspace(workspace, workspace_bytes, pages_workspace(pool));
+  if (rc != SHADOWKV_OK) return rc;
+  const hipError_t e = launch_pages_update(pool_arg(pool), parents, keep_lens, n_new, n_new_all, moves_arg(moves),
+                                           reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kAlign), static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SHADOWKV_OK : fail_hip("pages update", e);
+}
+
+int shadowkv_pages_compact(const shadowkv_page_pool* pool, int32_t max_moves, const shadowkv_page_moves* moves, int32_t* n_used, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  int rc = check_pool(pool, true);
+  if (rc == SHADOWKV_OK) rc = check_moves(moves);
+  if (rc != SHADOWKV_OK) return rc;
+  if (!moves->count || (moves->capacity > 0 && (!moves->src || !moves->dst))) return fail_inval("src, dst and count of moves must not be NULL");
+  if (max_moves < 0) return fail_inval("max_moves must be >= 0");
+  rc = check_workspace(workspace, workspace_bytes, pages_workspace(pool));
+  if (rc != SHADOWKV_OK) return rc;
+  int32_t* ws = static_cast<int32_t*>(workspace);
+  const hipError_t e = launch_pages_compact(pool_arg(pool), max_moves, moves_arg(moves), n_used, ws + kAlign / sizeof(int32_t), ws,
+                                            static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SHADOWKV_OK : fail_hip("pages compact", e);
+}
+
+int shadowkv_pages_copy(const shadowkv_paged_cache* const* from, const shadowkv_paged_cache* const* to, int32_t n_layers,
+                        const shadowkv_page_moves* moves, void* stream) {
+  int rc = check_moves(moves);
+  if (rc != SHADOWKV_OK) return rc;
+  if (n_layers < 0 || n_layers > 4096) return fail_inval("n_layers must be in [0, 4096]");
+  if (n_layers && (!from || !to)) return fail_inval("from and to must not be NULL");
+  if (moves->capacity > 0 && (!moves->src || !moves->dst)) return fail_inval("src and dst of moves must not be NULL");
+  for (int l = 0; l < n_layers; ++l) {
+    rc = check_pages(from[l], false);
+    if (rc == SHADOWKV_OK) rc = check_pages(to[l], true);
+    if (rc != SHADOWKV_OK) return rc;
+    if (from[l]->n_kv_heads != to[l]->n_kv_heads || from[l]->head_dim != to[l]->head_dim || from[l]->page_size != to[l]->page_size ||
+        from[l]->kv_dtype != to[l]->kv_dtype)
+      return fail_inval("layer %d: the caches differ in heads, page size or type", l);
+  }
+  if (moves->capacity == 0) return SHADOWKV_OK;
+  for (int l = 0; l < n_layers;) {
+    const shadowkv_paged_cache *f = from[l], *t = to[l];
+    const int eb = elem_bytes(f->kv_dtype);
+    PagesCopyArgs a{};
+    for (; l < n_layers && a.n_layers < kMaxCopyLayers && same_geometry(from[l], f) && same_geometry(to[l], t); ++l, ++a.n_layers) {
+      a.from_k[a.n_layers] = static_cast<const uint8_t*>(from[l]->k);
+      a.from_v[a.n_layers] = static_cast<const uint8_t*>(from[l]->v);
+      a.to_k[a.n_layers] = static_cast<uint8_t*>(to[l]->k);
+      a.to_v[a.n_layers] = static_cast<uint8_t*>(to[l]->v);
+    }
+    const int64_t st[4][3] = {{f->k_page_stride, f->k_head_stride, f->k_token_stride}, {f->v_page_stride, f->v_head_stride, f->v_token_stride},
+                              {t->k_page_stride, t->k_head_stride, t->k_token_stride}, {t->v_page_stride, t->v_head_stride, t->v_token_stride}};
+    for (int i = 0; i < 3; ++i) { a.fk[i] = st[0][i] * eb; a.fv[i] = st[1][i] * eb; a.tk[i] = st[2][i] * eb; a.tv[i] = st[3][i] * eb; }
+    a.hkv = f->n_kv_heads;
+    a.row_bytes = f->head_dim * eb;
+    a.page_size = f->page_size;
+    a.from_pages = f->n_pages;
+    a.to_pages = t->n_pages;
+    a.m = moves_arg(moves);
+    const hipError_t e = launch_pages_copy(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail_hip("pages copy", e);
+  }
+  return SHADOWKV_OK;
+}
 
 int shadowkv_rope_frequencies(const shadowkv_rope* rope, double* out) {
   double w[kMaxHalfDim];

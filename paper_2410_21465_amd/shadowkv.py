@@ -21,6 +21,7 @@ VALUES_DEVICE, VALUES_HOST = 0, 1
 FLAG_STAGE_VALUES = 1
 FLAG_KEEP_REBUILT_KEYS = 2
 KV_BF16, KV_FP8_E5M2 = 0, 1     # storage type of the KV-cache tensors (Params.kv_dtype)
+LOGITS_BF16, LOGITS_FP16, LOGITS_FP32 = 0, 1, 2
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1                                        # Rope.layout
 ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3, 4  # Rope.scaling
 
@@ -33,7 +34,9 @@ EXPORTS = (
     "shadowkv_factorize_keys", "shadowkv_factorize_workspace_bytes", "shadowkv_decode_step_static",
     "shadowkv_static_scratch_bytes", "shadowkv_decode_plan", "shadowkv_factorize_plan",
     "shadowkv_decode_score_rows", "shadowkv_rope_frequencies", "shadowkv_rotate", "shadowkv_paged_append",
-    "shadowkv_paged_attention", "shadowkv_paged_attention_workspace_bytes",
+    "shadowkv_paged_attention", "shadowkv_paged_attention_workspace_bytes", "shadowkv_beam_select",
+    "shadowkv_beam_select_workspace_bytes", "shadowkv_reorder_rows", "shadowkv_pages_update", "shadowkv_pages_compact",
+    "shadowkv_pages_workspace_bytes", "shadowkv_pages_copy",
 )
 STAGES = ("score", "select", "gather_values", "attention")
 
@@ -67,6 +70,26 @@ class CPagedCache(C.Structure):
                 ("page_table", C.c_void_p), ("table_stride", C.c_int64),
                 ("batch", C.c_int32), ("pages_per_seq", C.c_int32), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("page_size", C.c_int32), ("kv_dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class CLogits(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("group_stride", C.c_int64), ("beam_stride", C.c_int64), ("n_groups", C.c_int32),
+                ("n_beams", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32)]
+
+
+class CRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("outer_stride", C.c_int64), ("inner", C.c_int64),
+                ("n_outer", C.c_int32), ("reserved", C.c_int32)]
+
+
+class CPagePool(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("table_stride", C.c_int64), ("kv_lens", C.c_void_p), ("page_refs", C.c_void_p),
+                ("batch", C.c_int32), ("pages_per_seq", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32)]
+
+
+class CPageMoves(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("rows", C.c_void_p), ("count", C.c_void_p), ("capacity", C.c_int32),
+                ("reserved", C.c_int32)]
 
 
 class ShadowKVError(RuntimeError):
@@ -127,6 +150,20 @@ def lib() -> C.CDLL:
         L.shadowkv_paged_attention.argtypes = [vp] * 6 + [i32, C.c_double, vp, sz, vp]
         L.shadowkv_paged_attention_workspace_bytes.restype = sz
         L.shadowkv_paged_attention_workspace_bytes.argtypes = [vp, i32, i32]
+        L.shadowkv_beam_select.restype = i32
+        L.shadowkv_beam_select.argtypes = [vp] * 4 + [C.c_double, C.c_double, C.c_int32, C.c_int32] + [vp] * 6 + [sz, vp]
+        L.shadowkv_beam_select_workspace_bytes.restype = sz
+        L.shadowkv_beam_select_workspace_bytes.argtypes = [vp, C.c_int32]
+        L.shadowkv_reorder_rows.restype = i32
+        L.shadowkv_reorder_rows.argtypes = [vp, C.c_int32, vp, C.c_int32, vp]
+        L.shadowkv_pages_update.restype = i32
+        L.shadowkv_pages_update.argtypes = [vp] * 4 + [C.c_int32, vp, vp, sz, vp]
+        L.shadowkv_pages_compact.restype = i32
+        L.shadowkv_pages_compact.argtypes = [vp, C.c_int32, vp, vp, vp, sz, vp]
+        L.shadowkv_pages_workspace_bytes.restype = sz
+        L.shadowkv_pages_workspace_bytes.argtypes = [vp]
+        L.shadowkv_pages_copy.restype = i32
+        L.shadowkv_pages_copy.argtypes = [vp, vp, C.c_int32, vp, vp]
         L.shadowkv_build_workspace_bytes.restype = sz
         L.shadowkv_build_workspace_bytes.argtypes = [vp]
         L.shadowkv_decode_workspace_bytes.restype = sz
@@ -709,3 +746,192 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, kv_lens: torch.Tensor, s
                                               1 if causal else 0, float(softmax_scale), workspace.data_ptr(),
                                               workspace.numel() * workspace.element_size(), st))
     return out
+
+
+# ---- a search over several continuations: the choice over beams and vocabulary, and the state that follows it ----
+
+_LOGITS = {torch.bfloat16: LOGITS_BF16, torch.float16: LOGITS_FP16, torch.float32: LOGITS_FP32}
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, n_out: int = 0, finished: Optional[torch.Tensor] = None,
+                lengths: Optional[torch.Tensor] = None, length_penalty: float = 0.0, logit_scale: float = 0.0, end_token: int = -1,
+                out: Optional[dict] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
+    """The ``n_out`` (0: as many as beams) best continuations of every group from ``logits [groups, beams, vocab]`` (bf16, fp16 or
+    fp32; strides of groups and beams as they come) and the beams' summed log-probabilities ``scores [groups, beams]`` float32.
+    ``finished`` (bool) beams offer themselves; ranks are scores over (``lengths`` int32 + 1) ** ``length_penalty``.
+
+    Returns ``scores``, ``parents`` (rows ``group * beams + beam``; -1: nothing was left) and ``tokens [groups, n_out]`` in descending
+    order of rank; with ``finished`` or an ``end_token`` also ``finished``, with ``lengths`` also ``lengths``.  ``out`` may be such a
+    dict, whose scores, finished and lengths may be the arguments themselves where ``n_out`` is ``beams``."""
+    if logits.dim() != 3 or logits.dtype not in _LOGITS or not logits.is_cuda:
+        raise ValueError("logits must be a bfloat16, float16 or float32 tensor [groups, beams, vocab] on the GPU")
+    groups, beams, vocab = logits.shape
+    sg, sb, sv = logits.stride()
+    if vocab > 1 and sv != 1:
+        raise ValueError("the logits of a beam must be contiguous")
+    dev = logits.device
+    _want(scores, "scores", torch.float32, (groups, beams), dev)
+    if finished is not None:
+        _want(finished, "finished", torch.bool, (groups, beams), dev)
+    if lengths is not None:
+        _want(lengths, "lengths", torch.int32, (groups, beams), dev)
+    n = n_out or beams
+    c = CLogits(logits.data_ptr(), sg, sb, groups, beams, vocab, _LOGITS[logits.dtype])
+    need = int(lib().shadowkv_beam_select_workspace_bytes(C.byref(c), n))
+    if need == 0:
+        raise ShadowKVError(EINVAL, last_error())
+    kinds = {"scores": torch.float32, "parents": torch.int32, "tokens": torch.int32}
+    if finished is not None or end_token >= 0:
+        kinds["finished"] = torch.bool
+    if lengths is not None:
+        kinds["lengths"] = torch.int32
+    with _Launch(dev, stream) as st:
+        if out is None:
+            out = {name: torch.empty(groups, n, dtype=kind, device=dev) for name, kind in kinds.items()}
+        else:
+            if out.keys() != kinds.keys():
+                raise ValueError(f"out must have {', '.join(kinds)}")
+            for name, kind in kinds.items():
+                _want(out[name], name, kind, (groups, n), dev)
+        if workspace is None:
+            workspace = alloc_workspace(need, dev)
+        elif workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+        _check(lib().shadowkv_beam_select(
+            C.byref(c), scores.data_ptr(), None if finished is None else finished.data_ptr(), None if lengths is None else lengths.data_ptr(),
+            float(length_penalty), float(logit_scale), int(end_token), n, out["scores"].data_ptr(), out["parents"].data_ptr(),
+            out["tokens"].data_ptr(), out["finished"].data_ptr() if "finished" in out else None,
+            out["lengths"].data_ptr() if "lengths" in out else None, workspace.data_ptr(), workspace.numel() * workspace.element_size(), st))
+    return out
+
+
+def _rows(t: torch.Tensor, n: int, device) -> CRows:
+    """[rows, ...] as ``shadowkv_rows``: what follows the rows has to be pieces of contiguous elements at one stride."""
+    if t.dim() == 0 or t.shape[0] != n:
+        raise ValueError(f"an array must have {n} rows, not shape {tuple(t.shape)}")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"an array must be on {device}, not {t.device}")
+    eb, inner, outer, step = t.element_size(), 1, 1, 0
+    if t.numel() == 0:
+        return CRows(None, 0, 0, 0, 0, 0)
+    if t[0].is_contiguous():
+        return CRows(t.data_ptr(), t.stride(0) * eb, 0, t.numel() // n * eb, 1, 0)
+    dims = [(s, d) for s, d in zip(t.shape[1:], t.stride()[1:]) if s != 1]
+    while dims and dims[-1][1] == inner:
+        inner *= dims.pop()[0]
+    if dims:
+        outer, step = dims.pop()
+    while dims and dims[-1][1] == outer * step:
+        outer *= dims.pop()[0]
+    if dims:
+        raise ValueError(f"rows of shape {tuple(t.shape[1:])} and strides {t.stride()[1:]} are not pieces at one stride")
+    return CRows(t.data_ptr(), t.stride(0) * eb, step * eb, inner * eb, outer, 0)
+
+
+def reorder_rows(arrays, parents: torch.Tensor, stream=None) -> None:
+    """Row i of every tensor of ``arrays`` (one tensor or several, ``[rows, ...]`` of any types; views such as ``A[:, prompt:]`` or
+    ``k[:, :, -32:]`` too) becomes what row ``parents[i]`` was, in place.  ``parents`` int32, as many as rows (``[groups, beams]`` of
+    ``beam_select``, say); rows with a parent outside stay as they are."""
+    arrays = [arrays] if isinstance(arrays, torch.Tensor) else list(arrays)
+    n, dev = parents.numel(), parents.device
+    _want(parents, "parents", torch.int32, parents.shape)
+    rows = (CRows * max(len(arrays), 1))(*(_rows(t, n, dev) for t in arrays))
+    with _Launch(dev, stream) as st:
+        _check(lib().shadowkv_reorder_rows(rows, len(arrays), parents.data_ptr(), n, st))
+
+
+def _pages_copy(caches, to, moves: CPageMoves, st) -> None:
+    ptrs = C.POINTER(CPagedCache) * max(len(caches), 1)
+    frm = ptrs(*(C.pointer(c.c) for c in caches))
+    _check(lib().shadowkv_pages_copy(frm, frm if to is caches else ptrs(*(C.pointer(c.c) for c in to)), len(caches), C.byref(moves), st))
+
+
+def pages_copy(caches, src: torch.Tensor, dst: torch.Tensor, rows: Optional[torch.Tensor] = None, to=None, stream=None) -> None:
+    """Pages ``src [n]`` int32 of every cache of ``caches`` (one for each layer) to pages ``dst [n]`` of the same cache, or of its
+    counterpart in ``to``; with ``rows [n]`` int32 only the first so many tokens of each.  Numbers outside a cache are left out; no page may
+    be written twice, or be read and written."""
+    caches = [caches] if isinstance(caches, PagedCache) else list(caches)
+    to = caches if to is None else [to] if isinstance(to, PagedCache) else list(to)
+    if len(to) != len(caches):
+        raise ValueError(f"{len(caches)} caches go to {len(to)}")
+    dev = src.device
+    _want(src, "src", torch.int32, (src.numel(),))
+    _want(dst, "dst", torch.int32, src.shape, dev)
+    if rows is not None:
+        _want(rows, "rows", torch.int32, src.shape, dev)
+    if any(c.device != dev for c in caches) or any(c.device != dev for c in to):
+        raise ValueError(f"the caches must be on {dev}")
+    with _Launch(dev, stream) as st:
+        _pages_copy(caches, to, CPageMoves(src.data_ptr(), dst.data_ptr(), None if rows is None else rows.data_ptr(), None, src.numel(), 0), st)
+
+
+class PagePool:
+    """Who holds which page of ``n_pages``: ``page_table [batch, pages_per_seq]`` int32 (-1: no page), ``kv_lens [batch]`` int32 and
+    ``page_refs [n_pages]`` int32 (holders; 0: free), empty at first.  The caches of all layers share the table (``cache``).  A caller who
+    keeps pages for later adds to ``page_refs``, and subtracts when they are done with.
+
+    ``move_src``, ``move_dst``, ``move_rows`` and ``move_count`` are the copies that the last call asked for; the caches that it was given
+    have been copied."""
+
+    def __init__(self, batch: int, pages_per_seq: int, n_pages: int, page_size: int, device="cuda"):
+        c = CPagePool(None, pages_per_seq, None, None, batch, pages_per_seq, n_pages, page_size)
+        need = int(lib().shadowkv_pages_workspace_bytes(C.byref(c)))
+        if need == 0:
+            raise ShadowKVError(EINVAL, last_error())
+        self.batch, self.pages_per_seq, self.n_pages, self.page_size = batch, pages_per_seq, n_pages, page_size
+        ints = lambda n: torch.zeros(n, dtype=torch.int32, device=device)  # noqa: E731
+        self.page_table = torch.full((batch, pages_per_seq), -1, dtype=torch.int32, device=device)
+        self.kv_lens, self.page_refs = ints(batch), ints(n_pages)
+        self.device = self.page_table.device
+        room = max(batch, n_pages // 2 + 1)
+        self.move_src, self.move_dst, self.move_rows, self.move_count, self.n_used = ints(room), ints(room), ints(room), ints(1), ints(1)
+        self.workspace = alloc_workspace(need, self.device)
+        c.page_table, c.kv_lens, c.page_refs = self.page_table.data_ptr(), self.kv_lens.data_ptr(), self.page_refs.data_ptr()
+        self.c = c
+
+    def cache(self, k: torch.Tensor, v: torch.Tensor) -> PagedCache:
+        """``PagedCache`` of a layer's pages ``k, v [n_pages, h_kv, page_size, d]`` under this pool's table."""
+        if k.dim() != 4 or k.shape[0] != self.n_pages or k.shape[2] != self.page_size:
+            raise ValueError(f"k and v must be [{self.n_pages}, h_kv, {self.page_size}, d]")
+        return PagedCache(k, v, self.page_table)
+
+    def _layers(self, caches) -> list:
+        caches = [caches] if isinstance(caches, PagedCache) else list(caches)
+        for c in caches:
+            if c.device != self.device or c.c.page_size != self.page_size or c.c.n_pages < self.n_pages:
+                raise ValueError(f"a cache must have {self.n_pages} pages of {self.page_size} tokens on {self.device}")
+        return caches
+
+    def _moves(self, room: int) -> CPageMoves:
+        return CPageMoves(self.move_src.data_ptr(), self.move_dst.data_ptr(), self.move_rows.data_ptr(), self.move_count.data_ptr(), room, 0)
+
+    def update(self, parents: Optional[torch.Tensor] = None, keep_lens: Optional[torch.Tensor] = None, n_new=0, caches=(), stream=None) -> None:
+        """Row i becomes the first ``min(kv_lens[parents[i]], keep_lens[i])`` tokens of what row ``parents[i]`` was (empty where that is
+        outside the batch), with room for ``n_new`` (a number, or int32 ``[batch]``) further ones, which ``kv_lens`` then counts, as
+        ``paged_append`` wants it; a row that the pages do not suffice for gets none.  Copies, in every cache of ``caches``, the last pages that
+        rows share and are about to write."""
+        for name, t in (("parents", parents), ("keep_lens", keep_lens), ("n_new", n_new)):
+            if isinstance(t, torch.Tensor) and t.numel() != self.batch:
+                raise ValueError(f"{name} must have {self.batch} elements, not {t.numel()}")
+            if isinstance(t, torch.Tensor):
+                _want(t, name, torch.int32, t.shape, self.device)
+        each = isinstance(n_new, torch.Tensor)
+        caches, moves = self._layers(caches), self._moves(self.batch)
+        with _Launch(self.device, stream) as st:
+            _check(lib().shadowkv_pages_update(C.byref(self.c), None if parents is None else parents.data_ptr(),
+                                               None if keep_lens is None else keep_lens.data_ptr(), n_new.data_ptr() if each else None,
+                                               0 if each else int(n_new), C.byref(moves), self.workspace.data_ptr(), self.workspace.numel(), st))
+            if caches:
+                _pages_copy(caches, caches, moves, st)
+
+    def compact(self, max_moves: Optional[int] = None, caches=(), stream=None) -> torch.Tensor:
+        """Moves the highest used pages into the lowest free ones (at most ``max_moves``), in every cache of ``caches``.  Returns ``n_used [1]``
+        int32 on the device: all pages from there on are free."""
+        room = self.move_src.numel()
+        caches, moves = self._layers(caches), self._moves(room)
+        with _Launch(self.device, stream) as st:
+            _check(lib().shadowkv_pages_compact(C.byref(self.c), room if max_moves is None else int(max_moves), C.byref(moves), self.n_used.data_ptr(),
+                                                self.workspace.data_ptr(), self.workspace.numel(), st))
+            if caches:
+                _pages_copy(caches, caches, moves, st)
+        return self.n_used
