@@ -269,6 +269,7 @@ struct BeamArgs {
   int64_t group_stride, beam_stride;
   int groups, beams, vocab, dtype, n;
   int part_len, n_parts;    // tokens of a part (a multiple of 512), parts of a row
+  int n_blocks;             // blocks of 128 tokens of a row
   double scale, penalty;
   const float* scores;
   const uint8_t* finished;
@@ -279,9 +280,10 @@ struct BeamArgs {
   uint8_t* out_finished;
   int32_t* out_lengths;
   BeamPart* parts;          // [rows, n_parts]
-  uint2* best;              // [rows, n_parts, n] (logit as fp32 bits, token), descending; token ~0u: none
+  float* peaks;             // [rows, n_blocks] largest logit of a block
 };
 int beam_part_len(int64_t rows, int vocab);
+int beam_blocks(int vocab);
 hipError_t launch_beam_select(const BeamArgs& a, hipStream_t st);
 
 constexpr int kMaxReorderRows = 2048, kMaxReorderArrays = 64;

@@ -1,8 +1,9 @@
 // The n best continuations of every group of beams, by summed log-probability:
 //   score = s + c x_v - log sum_w exp(c x_w),   rank = score / length^a.
-// Two launches.  The first reads the logits once: a wave takes a part of a row and keeps the part's sum of exponentials (fp64, relative to a
-// logit of the part) and its n best logits in order.  The second, a workgroup per group, joins the parts of every row, forms the ranks of
-// what the rows offer, and keeps the n best of those.
+// Two launches.  The first reads the logits once: a wave takes a part of a row, sums its exponentials (fp64, relative to a logit of the
+// part) and keeps the largest logit of every block of 128 tokens, nothing else.  The second has a workgroup per group and a wave per row: the
+// n best tokens of a row lie in the n blocks with the largest maxima (whatever lies in another block has n better ones, one in each of
+// those), so it finds these, reads them again, and keeps their n best; then the first wave ranks what all rows offer.
 //
 // Ranks of different rows meet in the choice, so the sums are fp64: exp as 2^t = 2^round(t) 2^f, f in [-1/2, 1/2], with 2^f the Chebyshev
 // interpolation of degree 8 (off by 1.1e-12 at most), 2^round(t) added to the exponent's bits.  Lanes take the same tokens in the same
@@ -14,8 +15,9 @@
 namespace skv {
 namespace {
 
-constexpr int kElems = 8;                       // logits of a lane at a time
+constexpr int kElems = 8;                       // consecutive logits of a lane
 constexpr int kChunk = kWave * kElems;
+constexpr int kBlock = 16 * kElems;             // tokens of a block: a row of 16 lanes
 constexpr double kLog2e = 1.4426950408889634074;
 
 // 2^t for t in [-1000, 1000]
@@ -40,13 +42,6 @@ __device__ __forceinline__ uint32_t f32_key(float x) {   // larger value <=> lar
   return (u >> 31) ? ~u : (u | 0x80000000u);
 }
 __device__ __forceinline__ float key_f32(uint32_t k) { return __uint_as_float((k >> 31) ? (k & 0x7fffffffu) : ~k); }
-__device__ __forceinline__ uint64_t readlane_u64(uint64_t v, int lane) {
-  return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
-}
-__device__ __forceinline__ uint64_t from_lane_below(uint64_t v, int lane) {
-  const int src = lane > 0 ? lane - 1 : 0;
-  return ((uint64_t)(uint32_t)__shfl((int)(v >> 32), src, kWave) << 32) | (uint32_t)__shfl((int)(uint32_t)v, src, kWave);
-}
 __device__ __forceinline__ float wave_max_f32(float v) {
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m, kWave));
@@ -59,45 +54,40 @@ template <>
 struct Logit<SHADOWKV_LOGITS_BF16> {
   static constexpr int bytes = 2;
   static __device__ __forceinline__ float one(const uint8_t* p) { return bf16_to_f32(*reinterpret_cast<const uint16_t*>(p)); }
-  static __device__ __forceinline__ void unpack(const uint4& w, float* x) {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  static __device__ __forceinline__ void unpack(const uint32_t* w, float* x) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(u[i]); x[2 * i + 1] = bf16_hi(u[i]); }
+    for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
   }
 };
 template <>
 struct Logit<SHADOWKV_LOGITS_FP16> {
   static constexpr int bytes = 2;
   static __device__ __forceinline__ float one(const uint8_t* p) { return (float)*reinterpret_cast<const _Float16*>(p); }
-  static __device__ __forceinline__ void unpack(const uint4& w, float* x) {
-    typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-    const half8 h = __builtin_bit_cast(half8, w);
+  static __device__ __forceinline__ void unpack(const uint32_t* w, float* x) {
+    typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (float)h[i];
+    for (int i = 0; i < 4; ++i) {
+      const half2_t h = __builtin_bit_cast(half2_t, w[i]);
+      x[2 * i] = (float)h[0]; x[2 * i + 1] = (float)h[1];
+    }
   }
 };
 template <>
 struct Logit<SHADOWKV_LOGITS_FP32> {
   static constexpr int bytes = 4;
   static __device__ __forceinline__ float one(const uint8_t* p) { return *reinterpret_cast<const float*>(p); }
-  static __device__ __forceinline__ void unpack(const uint4& w, float* x) {
-    x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+  static __device__ __forceinline__ void unpack(const uint32_t* w, float* x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
   }
 };
 
 // whether a row takes part at all
 __device__ __forceinline__ bool row_lives(float score) { return fabsf(score) < INFINITY; }
 
-// c (the same in all lanes) into the wave's list of 64, lane i the i-th largest
-__device__ __forceinline__ void insert(uint64_t& list, uint64_t c, int lane) {
-  const int pos = __popcll(__ballot(list > c));
-  const uint64_t below = from_lane_below(list, lane);
-  list = lane < pos ? list : lane == pos ? c : below;
-}
-
 template <int DT>
 __global__ __launch_bounds__(256) void beam_parts_kernel(BeamArgs a) {
-  constexpr int EB = Logit<DT>::bytes, VEC = 16 / EB;
+  constexpr int EB = Logit<DT>::bytes, WORDS = kElems * EB / 4;
   const int lane = threadIdx.x & (kWave - 1);
   const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (w >= (int64_t)a.groups * a.beams * a.n_parts) return;
@@ -105,33 +95,46 @@ __global__ __launch_bounds__(256) void beam_parts_kernel(BeamArgs a) {
   if (!row_lives(a.scores[row]) || (a.finished && a.finished[row])) return;   // (the second launch asks the same)
   const uint8_t* p = a.logits + (row / a.beams) * a.group_stride + (row % a.beams) * a.beam_stride;
   const int t0 = part * a.part_len, t1 = min(a.vocab, t0 + a.part_len);
+  float* peak = a.peaks + (int64_t)row * a.n_blocks + t0 / kBlock;
   const double cl = a.scale * kLog2e;
-  float ref = -INFINITY, least = -INFINITY;     // least: what the list's n-th logit is
+  const float reach = (float)fmin(500.0 / cl, 1e38);
+  float ref = -INFINITY;
   double sum = 0.0;
   bool bad = false;
-  uint64_t list = 0;                            // (key of the logit, ~token); 0: nothing
-  for (int base = t0; base < t1; base += kChunk) {
-    float x[kElems];
+  uint32_t raw[WORDS];
+  auto load = [&](int base) {                   // (rows of an odd vocabulary begin at any element; behind the last one: minus infinity)
+    const int at = base + lane * kElems;
+    if (at + kElems <= t1) {
+      __builtin_memcpy(raw, p + (int64_t)at * EB, kElems * EB);
+    } else {
 #pragma unroll
-    for (int i = 0; i < kElems / VEC; ++i) {
-      const int at = base + (i * kWave + lane) * VEC;
-      if (at + VEC <= t1) {
-        uint4 v;
-        __builtin_memcpy(&v, p + (int64_t)at * EB, 16);      // (rows of an odd vocabulary begin at any element)
-        Logit<DT>::unpack(v, x + i * VEC);
-      } else {
+      for (int i = 0; i < WORDS; ++i) raw[i] = DT == SHADOWKV_LOGITS_BF16 ? 0xff80ff80u : DT == SHADOWKV_LOGITS_FP16 ? 0xfc00fc00u : 0xff800000u;
+      for (int e = 0; e < kElems; ++e) {
+        if (at + e >= t1) break;
+        if constexpr (EB == 4) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) x[i * VEC + e] = at + e < t1 ? Logit<DT>::one(p + (int64_t)(at + e) * EB) : -INFINITY;
+          for (int i = 0; i < WORDS; ++i)
+            if (i == e) raw[i] = *reinterpret_cast<const uint32_t*>(p + (int64_t)(at + e) * EB);
+        } else {
+          const uint32_t h = *reinterpret_cast<const uint16_t*>(p + (int64_t)(at + e) * EB);
+#pragma unroll
+          for (int i = 0; i < WORDS; ++i)
+            if (i == e / 2) raw[i] = e & 1 ? (raw[i] & 0xffffu) | (h << 16) : (raw[i] & 0xffff0000u) | h;
+        }
       }
     }
+  };
+  load(t0);
+  for (int base = t0; base < t1; base += kChunk) {
+    float x[kElems];
+    Logit<DT>::unpack(raw, x);
+    if (base + kChunk < t1) load(base + kChunk);
     float mx = x[0];
 #pragma unroll
-    for (int e = 0; e < kElems; ++e) {
-      bad |= __builtin_isnan(x[e]) || x[e] == INFINITY;
-      mx = fmaxf(mx, x[e]);
-    }
+    for (int e = 1; e < kElems; ++e) mx = __builtin_elementwise_maximum(mx, x[e]);   // (NaN if one is)
+    bad |= !(mx < INFINITY);
     // the reference moves up only where 2^t might leave fp64's range
-    if (__ballot(((double)mx - (double)ref) * cl > 500.0)) {
+    if (__ballot(mx > ref + reach)) {
       const float to = wave_max_f32(mx);
       sum *= exp2_f64(fmax(((double)ref - (double)to) * cl, -1000.0));
       ref = to;
@@ -140,48 +143,145 @@ __global__ __launch_bounds__(256) void beam_parts_kernel(BeamArgs a) {
 #pragma unroll
       for (int e = 0; e < kElems; ++e) sum += exp2_f64(fmax(((double)x[e] - (double)ref) * cl, -1000.0));
     }
-    if (__ballot(mx > least)) {                 // (a later token of an equal logit is not better)
-#pragma unroll
-      for (int e = 0; e < kElems; ++e) {
-        const uint32_t token = (uint32_t)(base + ((e / VEC) * kWave + lane) * VEC + e % VEC);
-        const uint64_t mine = ((uint64_t)f32_key(x[e]) << 32) | (uint32_t)~token;
-        uint64_t some = __ballot(x[e] >= least && x[e] > -INFINITY);
-        while (some) {
-          const int from = __ffsll((unsigned long long)some) - 1;
-          some &= some - 1;
-          const uint64_t c = readlane_u64(mine, from);
-          if (c > readlane_u64(list, a.n - 1)) insert(list, c, lane);
-        }
-        const uint64_t last = readlane_u64(list, a.n - 1);
-        least = last ? key_f32((uint32_t)(last >> 32)) : -INFINITY;
-      }
-    }
+    float m = mx;                               // lane 15 of 16 ends with the largest of them
+    m = fmaxf(m, __uint_as_float(dpp_u32<0x111>(__float_as_uint(m), __float_as_uint(m))));
+    m = fmaxf(m, __uint_as_float(dpp_u32<0x112>(__float_as_uint(m), __float_as_uint(m))));
+    m = fmaxf(m, __uint_as_float(dpp_u32<0x114>(__float_as_uint(m), __float_as_uint(m))));
+    m = fmaxf(m, __uint_as_float(dpp_u32<0x118>(__float_as_uint(m), __float_as_uint(m))));
+    const int block = (base - t0) / kBlock + lane / 16;
+    if (lane % 16 == 15 && block * kBlock < t1 - t0) peak[block] = m;
   }
   sum = wave_sum_f64_dpp(sum);
   const bool any_bad = __ballot(bad) != 0;
   if (lane == 0) a.parts[w] = BeamPart{sum, ref, any_bad};
-  if (lane < a.n) a.best[w * a.n + lane] = make_uint2(__float_as_uint(key_f32((uint32_t)(list >> 32))), list ? ~(uint32_t)list : ~0u);
 }
 
-// What a row offers, in LDS: candidate i is (logit, token); score = base + c (logit - ref).
+// ---- the n largest of many keys, by one wave ------------------------------------------------------------------------------
+// What reaches a bound that n keys reach, and few others do, is put into LDS in order of items and sorted by counting, for each, what is
+// larger (the earlier of equals first).
+constexpr int kSortRoom = 256;
+struct SortRoom {
+  uint64_t key[kSortRoom];
+  uint32_t item[kSortRoom];
+};
+// between writes and reads of LDS by different lanes of a wave
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+// the n-th largest of the lanes' keys (1 if that is 0, no key)
+__device__ __forceinline__ uint64_t lane_bound(uint64_t mine, int n, SortRoom& room, int lane) {
+  room.key[lane] = mine;
+  wave_sync();
+  int larger = 0;
+#pragma unroll 16
+  for (int j = 0; j < kWave; ++j) { const uint64_t k = room.key[j]; larger += k > mine || (k == mine && j < lane); }
+  const uint64_t bound = room.key[__ffsll((unsigned long long)__ballot(larger == n - 1)) - 1];
+  wave_sync();
+  return bound ? bound : 1;
+}
+// c: keys that have been taken, counted beyond the room as well
+__device__ __forceinline__ void take(uint64_t k, uint32_t item, bool takes, SortRoom& room, int& c, int lane) {
+  const uint64_t taken = __ballot(takes);
+  const int at = c + __popcll(taken & ((1ull << lane) - 1));
+  if (takes && at < kSortRoom) { room.key[at] = k; room.item[at] = item; }
+  c += __popcll(taken);
+}
+// the n best of the c <= kSortRoom in the room, in order; returns how many there are
+__device__ __forceinline__ int sort_room(SortRoom& room, int c, int n, uint64_t* keys, uint32_t* items, int lane) {
+  wave_sync();
+  for (int i = lane; i < c; i += kWave) {
+    const uint64_t k = room.key[i];
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < c; ++j) { const uint64_t o = room.key[j]; rank += o > k || (o == k && j < i); }
+    if (rank < n) { keys[rank] = k; items[rank] = room.item[i]; }
+  }
+  wave_sync();
+  return min(c, n);
+}
+// Where more than the room reach a bound (many equal keys, say): the largest bound that n keys reach, bit by bit, and of the
+// keys that equal it the first.  key(i): of item i < n_items, 0: none.
+template <int BITS, class Key>
+__device__ __forceinline__ int take_exactly(Key key, int n_items, int n, uint64_t bound, SortRoom& room, int lane) {
+  auto count = [&](uint64_t from) {
+    int c = 0;
+    for (int i0 = 0; i0 < n_items; i0 += kWave) c += __popcll(__ballot(i0 + lane < n_items && key(i0 + lane) >= from));
+    return c;
+  };
+  for (int b = BITS - 1; b >= 0; --b) {
+    const uint64_t up = (bound >> b | 1ull) << b;         // (bits above b are right; where bit b is set already this is not more)
+    const int reach = up > bound ? count(up) : 0;
+    if (reach >= n) bound = up;
+    if (reach == n) break;
+  }
+  const int spare = n - count(bound + 1);
+  int c = 0, equal = 0;
+  wave_sync();
+  for (int i0 = 0; i0 < n_items; i0 += kWave) {
+    const uint64_t k = i0 + lane < n_items ? key(i0 + lane) : 0, same = __ballot(k == bound);
+    take(k, (uint32_t)(i0 + lane), k > bound || (k == bound && equal + __popcll(same & ((1ull << lane) - 1)) < spare), room, c, lane);
+    equal += __popcll(same);
+  }
+  return c;
+}
+// the n largest of key(i), i < n_items, equals in order of items
+template <class K, class Key>
+__device__ __forceinline__ int top_items(Key key, int n_items, int n, SortRoom& room, uint64_t* keys, uint32_t* items, int lane) {
+  constexpr int kHeld = 16;                               // keys of a lane at a time
+  K held[kHeld], mine = 0;
+  const int step = kHeld * kWave;
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e) { const int i = i0 + e * kWave + lane; held[e] = i < n_items ? key(i) : 0; }
+  };
+  for (int i0 = 0; i0 < n_items; i0 += step) {
+    load(i0);
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e) mine = held[e] > mine ? held[e] : mine;
+  }
+  const uint64_t bound = lane_bound(mine, n, room, lane);
+  int c = 0;
+  for (int i0 = 0; i0 < n_items; i0 += step) {
+    if (n_items > step) load(i0);
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e)
+      if (i0 + e * kWave < n_items) take(held[e], (uint32_t)(i0 + e * kWave + lane), held[e] >= bound, room, c, lane);
+  }
+  if (c > kSortRoom) c = take_exactly<sizeof(K) * 8>(key, n_items, n, bound, room, lane);
+  return sort_room(room, c, n, keys, items, lane);
+}
+
+// What a row offers: candidate i is (logit, token); score = base + c (logit - ref).
 struct RowOffer {
-  double base, weight;                          // weight: length^penalty
+  double base;
   float ref;
   int count;
 };
+struct JoinWave {
+  SortRoom room;
+  uint64_t keys[64];
+  uint32_t items[64];
+};
 
-__global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
+template <int DT>
+__global__ __launch_bounds__(1024) void beam_join_kernel(BeamArgs a) {
+  constexpr int EB = Logit<DT>::bytes, WORDS = kElems * EB / 4, kAtOnce = kWave / 16;   // blocks that a wave reads at a time
   extern __shared__ __align__(16) uint8_t lds[];
-  RowOffer* offer = reinterpret_cast<RowOffer*>(lds);                        // [beams]
-  uint2* cand = reinterpret_cast<uint2*>(offer + a.beams);                   // [beams, n]
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, group = blockIdx.x;
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, waves = blockDim.x >> 6, group = blockIdx.x;
+  JoinWave& mine = reinterpret_cast<JoinWave*>(lds)[wave];
+  uint64_t* rank = reinterpret_cast<uint64_t*>(lds + waves * sizeof(JoinWave));    // [beams, n] keys of the ranks, 0: none
+  uint2* cand = reinterpret_cast<uint2*>(rank + a.beams * a.n);                    // [beams, n]
+  RowOffer* offer = reinterpret_cast<RowOffer*>(cand + a.beams * a.n);             // [beams]
   const double cl = a.scale * kLog2e;
-  for (int b = wave; b < a.beams; b += 4) {
+  for (int b = wave; b < a.beams; b += waves) {
     const int row = group * a.beams + b;
     const float s = a.scores[row];
     const bool done = a.finished && a.finished[row];
-    RowOffer o{(double)s, 1.0, 0.f, 0};
-    if (a.penalty != 0.0) o.weight = pow(fmax((double)a.lengths[row] + (done ? 0.0 : 1.0), 1.0), a.penalty);
+    double weight = 1.0;
+    if (a.penalty != 0.0) weight = pow(fmax((double)a.lengths[row] + (done ? 0.0 : 1.0), 1.0), a.penalty);
+    RowOffer o{(double)s, 0.f, 0};
     if (row_lives(s) && done) {
       o.count = 1;
       if (lane == 0) cand[b * a.n] = make_uint2(0u, (uint32_t)a.end_token);
@@ -192,79 +292,72 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
       for (int i = lane; i < a.n_parts; i += kWave) { bad |= parts[i].bad != 0; ref = fmaxf(ref, parts[i].ref); }
       ref = wave_max_f32(ref);
       if (!__ballot(bad) && ref > -INFINITY) {
+        const float* peak = a.peaks + (int64_t)row * a.n_blocks;
+        const int n_best = top_items<uint32_t>([&](int i) { const float x = peak[i]; return x > -INFINITY ? f32_key(x) : 0u; }, a.n_blocks, a.n,
+                                         mine.room, mine.keys, mine.items, lane);
         double sum = 0.0;
         for (int i = lane; i < a.n_parts; i += kWave)
           if (parts[i].ref > -INFINITY) sum += parts[i].sum * exp2_f64(fmax(((double)parts[i].ref - (double)ref) * cl, -1000.0));
         sum = wave_sum_f64_dpp(sum);
         o.base = (double)s - log(sum);
         o.ref = ref;
-        // the n best of the parts' lists, best places first
-        const uint2* best = a.best + (int64_t)row * a.n_parts * a.n;
-        uint64_t list = 0;
-        for (int place = 0; place < a.n; ++place)
-          for (int i0 = 0; i0 < a.n_parts; i0 += kWave) {
-            uint64_t mine = 0;
-            if (i0 + lane < a.n_parts) {
-              const uint2 c = best[(int64_t)(i0 + lane) * a.n + place];
-              if (c.y != ~0u) mine = ((uint64_t)f32_key(__uint_as_float(c.x)) << 32) | (uint32_t)~c.y;
+        // tokens of those blocks that are not less than the n-th block's largest (of fewer blocks: than the n-th lane's)
+        const uint8_t* p = a.logits + group * a.group_stride + b * a.beam_stride;
+        auto key_of = [&](float x, int t) { return x > -INFINITY ? ((uint64_t)f32_key(x) << 32) | (uint32_t)~t : 0ull; };
+        auto each_token = [&](auto f) {
+          for (int i0 = 0; i0 < n_best; i0 += kAtOnce) {
+            const int i = i0 + lane / 16;
+            const int at = i < n_best ? (int)mine.items[i] * kBlock + lane % 16 * kElems : a.vocab;
+            float x[kElems];
+            if (at + kElems <= a.vocab) {
+              uint32_t raw[WORDS];
+              __builtin_memcpy(raw, p + (int64_t)at * EB, kElems * EB);
+              Logit<DT>::unpack(raw, x);
+            } else {
+#pragma unroll
+              for (int e = 0; e < kElems; ++e) x[e] = at + e < a.vocab ? Logit<DT>::one(p + (int64_t)(at + e) * EB) : -INFINITY;
             }
-            uint64_t some = __ballot(mine > readlane_u64(list, a.n - 1));
-            while (some) {
-              const int from = __ffsll((unsigned long long)some) - 1;
-              some &= some - 1;
-              const uint64_t c = readlane_u64(mine, from);
-              if (c > readlane_u64(list, a.n - 1)) insert(list, c, lane);
-            }
+#pragma unroll
+            for (int e = 0; e < kElems; ++e) f(key_of(x[e], at + e));
           }
-        o.count = __popcll(__ballot(lane < a.n && list != 0));
-        if (lane < a.n) cand[b * a.n + lane] = make_uint2(__float_as_uint(key_f32((uint32_t)(list >> 32))), ~(uint32_t)list);
+        };
+        uint64_t bound;
+        if (n_best == a.n) {
+          bound = mine.keys[n_best - 1] << 32;
+        } else {
+          uint64_t best = 0;
+          each_token([&](uint64_t k) { best = k > best ? k : best; });
+          bound = lane_bound(best, a.n, mine.room, lane);
+        }
+        int c = 0;
+        each_token([&](uint64_t k) { if (__ballot(k >= bound)) take(k, 0, k >= bound, mine.room, c, lane); });
+        if (c > kSortRoom)
+          c = take_exactly<64>([&](int i) -> uint64_t {
+            const int t = (int)mine.items[i / kBlock] * kBlock + i % kBlock;
+            return t < a.vocab ? key_of(Logit<DT>::one(p + (int64_t)t * EB), t) : 0;
+          }, n_best * kBlock, a.n, bound, mine.room, lane);
+        o.count = sort_room(mine.room, c, a.n, mine.keys, mine.items, lane);
+        if (lane < o.count) cand[b * a.n + lane] = make_uint2(__float_as_uint(key_f32((uint32_t)(mine.keys[lane] >> 32))), ~(uint32_t)mine.keys[lane]);
       }
     }
+    wave_sync();
     if (lane == 0) offer[b] = o;
+    if (lane < a.n) rank[b * a.n + lane] = lane < o.count ? f64_key((o.base + a.scale * ((double)__uint_as_float(cand[b * a.n + lane].x) - (double)o.ref)) / weight) : 0;
   }
   __syncthreads();
   if (wave) return;
-  // ranks of all rows' candidates, best places first; lane i holds the i-th best: key of the rank, and (row, place) upside down
-  uint64_t key = 0;
-  uint32_t who = 0;
-  for (int place = 0; place < a.n; ++place)
-    for (int b0 = 0; b0 < a.beams; b0 += kWave) {
-      uint64_t k = 0;
-      uint32_t o = 0;
-      if (b0 + lane < a.beams) {
-        const int b = b0 + lane;
-        if (place < offer[b].count) {
-          const double score = offer[b].base + a.scale * ((double)__uint_as_float(cand[b * a.n + place].x) - (double)offer[b].ref);
-          k = f64_key(score / offer[b].weight);
-          o = ~(uint32_t)(b * 64 + place);
-        }
-      }
-      uint64_t last = readlane_u64(key, a.n - 1);
-      uint32_t last_who = (uint32_t)__builtin_amdgcn_readlane((int)who, a.n - 1);
-      uint64_t some = __ballot(k > last || (k == last && o > last_who));
-      while (some) {
-        const int from = __ffsll((unsigned long long)some) - 1;
-        some &= some - 1;
-        const uint64_t ck = readlane_u64(k, from);
-        const uint32_t co = (uint32_t)__builtin_amdgcn_readlane((int)o, from);
-        const int pos = __popcll(__ballot(key > ck || (key == ck && who > co)));
-        const uint64_t key_below = from_lane_below(key, lane);
-        const uint32_t who_below = (uint32_t)__shfl((int)who, lane > 0 ? lane - 1 : 0, kWave);
-        key = lane < pos ? key : lane == pos ? ck : key_below;
-        who = lane < pos ? who : lane == pos ? co : who_below;
-      }
-    }
+  // of all rows' candidates, in order of rows and places
+  const int count = top_items<uint64_t>([&](int i) { return rank[i]; }, a.beams * a.n, a.n, mine.room, mine.keys, mine.items, lane);
   // (all that this group's rows held has been read before anything is written: the outputs may be the inputs)
   float out_s = -INFINITY;
   int parent = -1, token = -1, length = 0;
   bool ended = false;
-  if (lane < a.n && key) {
-    const int b = (int)(~who >> 6), place = (int)(~who & 63u), row = group * a.beams + b;
-    const uint2 c = cand[b * a.n + place];
+  if (lane < count) {
+    const int i = (int)mine.items[lane], b = i / a.n, row = group * a.beams + b;
     const bool was = a.finished && a.finished[row];
-    out_s = (float)(offer[b].base + a.scale * ((double)__uint_as_float(c.x) - (double)offer[b].ref));
+    out_s = (float)(offer[b].base + a.scale * ((double)__uint_as_float(cand[i].x) - (double)offer[b].ref));
     parent = row;
-    token = (int)c.y;
+    token = (int)cand[i].y;
     ended = was || (a.end_token >= 0 && token == a.end_token);
     if (a.out_lengths) length = a.lengths[row] + (was ? 0 : 1);
   }
@@ -279,26 +372,37 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
   }
 }
 
+template <int DT>
+hipError_t launch(const BeamArgs& a, hipStream_t st) {
+  const int64_t waves = (int64_t)a.groups * a.beams * a.n_parts;
+  beam_parts_kernel<DT><<<dim3((unsigned)((waves + 3) / 4)), 256, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int join = a.beams < 16 ? a.beams : 16;
+  const size_t lds = join * sizeof(JoinWave) + (size_t)a.beams * (sizeof(RowOffer) + a.n * (sizeof(uint2) + sizeof(uint64_t)));
+  if (lds > 65536) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(&beam_join_kernel<DT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  beam_join_kernel<DT><<<dim3((unsigned)a.groups), join * kWave, lds, st>>>(a);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 int beam_part_len(int64_t rows, int vocab) {
-  (void)rows; (void)vocab;
-  return 2048;
+  const int64_t all = rows * (((int64_t)vocab + kChunk - 1) / kChunk);   // chunks
+  const int64_t per = (all + 8191) / 8192;
+  return (int)(per < 1 ? 1 : per > 1024 ? 1024 : per) * kChunk;
 }
+int beam_blocks(int vocab) { return (int)(((int64_t)vocab + kBlock - 1) / kBlock); }
 
 hipError_t launch_beam_select(const BeamArgs& a, hipStream_t st) {
-  const int64_t waves = (int64_t)a.groups * a.beams * a.n_parts;
-  const dim3 grid((unsigned)((waves + 3) / 4));
   switch (a.dtype) {
-    case SHADOWKV_LOGITS_BF16: beam_parts_kernel<SHADOWKV_LOGITS_BF16><<<grid, 256, 0, st>>>(a); break;
-    case SHADOWKV_LOGITS_FP16: beam_parts_kernel<SHADOWKV_LOGITS_FP16><<<grid, 256, 0, st>>>(a); break;
-    default: beam_parts_kernel<SHADOWKV_LOGITS_FP32><<<grid, 256, 0, st>>>(a); break;
+    case SHADOWKV_LOGITS_BF16: return launch<SHADOWKV_LOGITS_BF16>(a, st);
+    case SHADOWKV_LOGITS_FP16: return launch<SHADOWKV_LOGITS_FP16>(a, st);
+    default: return launch<SHADOWKV_LOGITS_FP32>(a, st);
   }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const size_t lds = (size_t)a.beams * (sizeof(RowOffer) + a.n * sizeof(uint2));
-  beam_join_kernel<<<dim3((unsigned)a.groups), 256, lds, st>>>(a);
-  return hipGetLastError();
 }
 
 }  // namespace skv

@@ -41,17 +41,17 @@ struct Span {
 bool meet(const Span& a, const Span& b) { return a.p && b.p && a.n && b.n && a.p < b.p + b.n && b.p < a.p + a.n; }
 
 struct BeamLayout {
-  int part_len, n_parts;
-  size_t best, total;
+  int part_len, n_parts, n_blocks;
+  size_t peaks, total;
 };
-BeamLayout beam_layout(const shadowkv_logits* x, int n_out) {
+BeamLayout beam_layout(const shadowkv_logits* x) {
   BeamLayout L;
   const int64_t rows = (int64_t)x->n_groups * x->n_beams;
   L.part_len = beam_part_len(rows, x->vocab);
   L.n_parts = (int)(((int64_t)x->vocab + L.part_len - 1) / L.part_len);
-  L.best = up((size_t)rows * L.n_parts * sizeof(BeamPart));
-  L.total = L.best + up((size_t)rows * L.n_parts * n_out * sizeof(uint2));
-  L.total = std::max(L.total, kAlign);
+  L.n_blocks = beam_blocks(x->vocab);
+  L.peaks = up((size_t)rows * L.n_parts * sizeof(BeamPart));
+  L.total = std::max(L.peaks + up((size_t)rows * L.n_blocks * sizeof(float)), kAlign);
   return L;
 }
 
@@ -80,7 +80,7 @@ struct Pieces {
 extern "C" {
 
 size_t shadowkv_beam_select_workspace_bytes(const shadowkv_logits* logits, int32_t n_out) {
-  return check_logits(logits, n_out, false) == SHADOWKV_OK ? beam_layout(logits, n_out).total : 0;
+  return check_logits(logits, n_out, false) == SHADOWKV_OK ? beam_layout(logits).total : 0;
 }
 
 int shadowkv_beam_select(const shadowkv_logits* logits, const float* scores, const uint8_t* finished, const int32_t* lengths, double length_penalty,
@@ -110,7 +110,7 @@ int shadowkv_beam_select(const shadowkv_logits* logits, const float* scores, con
     for (int j = 0; j < i; ++j)
       if (meet(outs[i], outs[j])) return fail_inval("outputs share memory with each other or the workspace");
   }
-  const BeamLayout L = beam_layout(logits, n_out);
+  const BeamLayout L = beam_layout(logits);
   rc = check_workspace(workspace, workspace_bytes, L.total);
   if (rc != SHADOWKV_OK) return rc;
   BeamArgs a{};
@@ -124,7 +124,8 @@ int shadowkv_beam_select(const shadowkv_logits* logits, const float* scores, con
   a.end_token = end_token;
   a.out_scores = out_scores; a.out_parents = out_parents; a.out_tokens = out_tokens; a.out_finished = out_finished; a.out_lengths = out_lengths;
   a.parts = static_cast<BeamPart*>(workspace);
-  a.best = reinterpret_cast<uint2*>(static_cast<char*>(workspace) + L.best);
+  a.n_blocks = L.n_blocks;
+  a.peaks = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.peaks);
   const hipError_t e = launch_beam_select(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SHADOWKV_OK : fail_hip("beam select", e);
 }
