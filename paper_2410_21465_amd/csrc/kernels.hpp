@@ -259,17 +259,17 @@ int paged_attn_workgroups();
 hipError_t launch_paged_attention(PagedAttnArgs a, int block_rows, hipStream_t st);
 
 // ---- a search over several continuations (kernels_beam.hip, kernels_reorder.hip, kernels_pages.hip) ----
-struct BeamPart {           // of a row: sum over a part of exp(c (x - ref)); bad: a logit is NaN or plus infinity
-  double sum;
-  float ref;                // -inf: no logit above minus infinity
-  int bad;
+struct BeamPart {           // of a row: sums over a part of exp(c x), and of exp(c (x - ref)) over chunks where those leave fp64's range
+  double plain, sum;
+  float ref;                // -inf: no such logit above minus infinity
+  int bad;                  // a logit is NaN or plus infinity
 };
 struct BeamArgs {
   const uint8_t* logits;    // strides in bytes
   int64_t group_stride, beam_stride;
   int groups, beams, vocab, dtype, n;
-  int part_len, n_parts;    // tokens of a part (a multiple of 512), parts of a row
-  int n_blocks;             // blocks of 128 tokens of a row
+  int part_len, n_parts;    // tokens of a part (a multiple of 1024), parts of a row
+  int n_blocks;             // blocks of 256 tokens of a row
   double scale, penalty;
   const float* scores;
   const uint8_t* finished;
@@ -280,7 +280,7 @@ struct BeamArgs {
   uint8_t* out_finished;
   int32_t* out_lengths;
   BeamPart* parts;          // [rows, n_parts]
-  float* peaks;             // [rows, n_blocks] largest logit of a block
+  uint32_t* peaks;          // [rows, n_blocks] largest logit of a block, as a key
 };
 int beam_part_len(int64_t rows, int vocab);
 int beam_blocks(int vocab);

@@ -1,13 +1,15 @@
 // The n best continuations of every group of beams, by summed log-probability:
 //   score = s + c x_v - log sum_w exp(c x_w),   rank = score / length^a.
-// Two launches.  The first reads the logits once: a wave takes a part of a row, sums its exponentials (fp64, relative to a logit of the
-// part) and keeps the largest logit of every block of 128 tokens, nothing else.  The second has a workgroup per group and a wave per row: the
+// Two launches.  The first reads the logits once: a wave takes a part of a row, sums its exponentials (fp64) and keeps the largest logit of
+// every block of 256 tokens, nothing else.  The second has a workgroup per group and a wave per row: the
 // n best tokens of a row lie in the n blocks with the largest maxima (whatever lies in another block has n better ones, one in each of
 // those), so it finds these, reads them again, and keeps their n best; then the first wave ranks what all rows offer.
 //
 // Ranks of different rows meet in the choice, so the sums are fp64: exp as 2^t = 2^round(t) 2^f, f in [-1/2, 1/2], with 2^f the Chebyshev
 // interpolation of degree 8 (off by 1.1e-12 at most), 2^round(t) added to the exponent's bits.  Lanes take the same tokens in the same
 // order in every row, whatever its address is, so rows of equal logits get equal sums.
+#include <algorithm>
+
 #include "../../include/shadowkv.h"
 #include "common.hpp"
 #include "kernels.hpp"
@@ -15,25 +17,48 @@
 namespace skv {
 namespace {
 
-constexpr int kElems = 8;                       // consecutive logits of a lane
+constexpr int kElems = 16;                      // consecutive logits of a lane
+constexpr int kTogether = 4;                    // of which so many exponentials are formed in step
 constexpr int kChunk = kWave * kElems;
 constexpr int kBlock = 16 * kElems;             // tokens of a block: a row of 16 lanes
 constexpr double kLog2e = 1.4426950408889634074;
 
-// 2^t for t in [-1000, 1000]
+// 2^f for f in [-1/2, 1/2], times 2^n
+constexpr double kExp2[9] = {1.3255179556479267e-06, 1.5310080611926545e-05, 0.00015403456082633648, 0.0013333450563173552, 0.009618129159053034,
+                             0.055504109412108156, 0.24022650695814518, 0.6931471805459332, 1.0000000000000004};
+__device__ __forceinline__ double exp2_frac(double f, int n) {
+  double p = fma(kExp2[0], f, kExp2[1]);
+#pragma unroll
+  for (int k = 2; k < 9; ++k) p = fma(p, f, kExp2[k]);
+  return __hiloint2double(__double2hiint(p) + (n << 20), __double2loint(p));
+}
+constexpr double kRound = 6755399441055744.0;   // 1.5 2^52: the low bits of t + kRound are round(t)
+// 2^t, t held to at least -1000
 __device__ __forceinline__ double exp2_f64(double t) {
-  const double big = 6755399441055744.0;        // 1.5 2^52: the low bits of t + big are round(t)
-  const double a = t + big, f = t - (a - big);
-  double p = 1.3255179556479267e-06;
-  p = fma(p, f, 1.5310080611926545e-05);
-  p = fma(p, f, 0.00015403456082633648);
-  p = fma(p, f, 0.0013333450563173552);
-  p = fma(p, f, 0.009618129159053034);
-  p = fma(p, f, 0.055504109412108156);
-  p = fma(p, f, 0.24022650695814518);
-  p = fma(p, f, 0.6931471805459332);
-  p = fma(p, f, 1.0000000000000004);
-  return __hiloint2double(__double2hiint(p) + (__double2loint(a) << 20), __double2loint(p));
+  t = fmax(t, -1000.0);
+  const double a = t + kRound;
+  return exp2_frac(t - (a - kRound), __double2loint(a));
+}
+// sum + 2^(x_0 c) + ... of N logits, |x c| < 1000 (the products are never rounded), in step with each other
+template <int N>
+__device__ __forceinline__ double add_exp2_of_products(double sum, const float* x, double c) {
+  double f[N], p[N];
+  int n[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const double a = fma((double)x[i], c, kRound);
+    n[i] = __double2loint(a);
+    f[i] = fma((double)x[i], c, -(a - kRound));
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) p[i] = fma(kExp2[0], f[i], kExp2[1]);
+#pragma unroll
+  for (int k = 2; k < 9; ++k)
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = fma(p[i], f[i], kExp2[k]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum += __hiloint2double(__double2hiint(p[i]) + (n[i] << 20), __double2loint(p[i]));
+  return sum;
 }
 
 __device__ __forceinline__ uint32_t f32_key(float x) {   // larger value <=> larger key, never 0 but for NaN
@@ -41,6 +66,7 @@ __device__ __forceinline__ uint32_t f32_key(float x) {   // larger value <=> lar
   const uint32_t u = __float_as_uint(x);
   return (u >> 31) ? ~u : (u | 0x80000000u);
 }
+constexpr uint32_t kLowestKey = 0x007fffffu;             // of minus infinity
 __device__ __forceinline__ float key_f32(uint32_t k) { return __uint_as_float((k >> 31) ? (k & 0x7fffffffu) : ~k); }
 __device__ __forceinline__ float wave_max_f32(float v) {
 #pragma unroll
@@ -54,19 +80,21 @@ template <>
 struct Logit<SHADOWKV_LOGITS_BF16> {
   static constexpr int bytes = 2;
   static __device__ __forceinline__ float one(const uint8_t* p) { return bf16_to_f32(*reinterpret_cast<const uint16_t*>(p)); }
+  template <int N>
   static __device__ __forceinline__ void unpack(const uint32_t* w, float* x) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
+    for (int i = 0; i < N / 2; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
   }
 };
 template <>
 struct Logit<SHADOWKV_LOGITS_FP16> {
   static constexpr int bytes = 2;
   static __device__ __forceinline__ float one(const uint8_t* p) { return (float)*reinterpret_cast<const _Float16*>(p); }
+  template <int N>
   static __device__ __forceinline__ void unpack(const uint32_t* w, float* x) {
     typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N / 2; ++i) {
       const half2_t h = __builtin_bit_cast(half2_t, w[i]);
       x[2 * i] = (float)h[0]; x[2 * i + 1] = (float)h[1];
     }
@@ -76,84 +104,122 @@ template <>
 struct Logit<SHADOWKV_LOGITS_FP32> {
   static constexpr int bytes = 4;
   static __device__ __forceinline__ float one(const uint8_t* p) { return *reinterpret_cast<const float*>(p); }
+  template <int N>
   static __device__ __forceinline__ void unpack(const uint32_t* w, float* x) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+    for (int i = 0; i < N; ++i) x[i] = __uint_as_float(w[i]);
   }
 };
 
 // whether a row takes part at all
 __device__ __forceinline__ bool row_lives(float score) { return fabsf(score) < INFINITY; }
 
+// Logits x with -800 < x c < 900 (c in units of log 2) are summed as they are, 2^(x c); a chunk with others (masks, infinities, logits far apart)
+// is summed relative to a logit that it or an earlier one holds, in a sum of its own.
+struct BeamScale {
+  double c;
+  float low, high;                              // x between them
+  float absent;                                 // adds 2^-900: what stands behind the last token
+};
+__device__ __forceinline__ BeamScale beam_scale(double scale) {
+  BeamScale s;
+  s.c = scale * kLog2e;
+  const bool fits = s.c > 0x1p-60 && s.c < 0x1p60;   // (else the borders leave fp32's range)
+  s.low = fits ? (float)(-800.0 / s.c) : INFINITY;
+  s.high = fits ? (float)(900.0 / s.c) : -INFINITY;
+  s.absent = fits ? (float)(-900.0 / s.c) : -INFINITY;
+  return s;
+}
+
 template <int DT>
-__global__ __launch_bounds__(256) void beam_parts_kernel(BeamArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6, 6))) void beam_parts_kernel(BeamArgs a) {
   constexpr int EB = Logit<DT>::bytes, WORDS = kElems * EB / 4;
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (w >= (int64_t)a.groups * a.beams * a.n_parts) return;
-  const int row = (int)(w / a.n_parts), part = (int)(w % a.n_parts);
+  const uint32_t w = blockIdx.x * 4 + (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  if (w >= (uint32_t)(a.groups * a.beams) * (uint32_t)a.n_parts) return;
+  const int row = (int)(w / (uint32_t)a.n_parts), part = (int)(w % (uint32_t)a.n_parts);
   if (!row_lives(a.scores[row]) || (a.finished && a.finished[row])) return;   // (the second launch asks the same)
   const uint8_t* p = a.logits + (row / a.beams) * a.group_stride + (row % a.beams) * a.beam_stride;
   const int t0 = part * a.part_len, t1 = min(a.vocab, t0 + a.part_len);
-  float* peak = a.peaks + (int64_t)row * a.n_blocks + t0 / kBlock;
-  const double cl = a.scale * kLog2e;
-  const float reach = (float)fmin(500.0 / cl, 1e38);
-  float ref = -INFINITY;
-  double sum = 0.0;
-  bool bad = false;
+  uint32_t* peak = a.peaks + (int64_t)row * a.n_blocks + t0 / kBlock;
+  const BeamScale sc = beam_scale(a.scale);
+  const float reach = (float)fmin(500.0 / sc.c, 1e38);
   uint32_t raw[WORDS];
-  auto load = [&](int base) {                   // (rows of an odd vocabulary begin at any element; behind the last one: minus infinity)
-    const int at = base + lane * kElems;
-    if (at + kElems <= t1) {
+  // rows of an odd vocabulary begin at any element; a lane that the end cuts off reads the last kElems tokens
+  auto load = [&](int base) {
+    const int at = min(base + lane * kElems, t1 - kElems);
+    if (a.vocab >= kElems) {
       __builtin_memcpy(raw, p + (int64_t)at * EB, kElems * EB);
     } else {
-#pragma unroll
-      for (int i = 0; i < WORDS; ++i) raw[i] = DT == SHADOWKV_LOGITS_BF16 ? 0xff80ff80u : DT == SHADOWKV_LOGITS_FP16 ? 0xfc00fc00u : 0xff800000u;
-      for (int e = 0; e < kElems; ++e) {
-        if (at + e >= t1) break;
-        if constexpr (EB == 4) {
-#pragma unroll
-          for (int i = 0; i < WORDS; ++i)
-            if (i == e) raw[i] = *reinterpret_cast<const uint32_t*>(p + (int64_t)(at + e) * EB);
-        } else {
-          const uint32_t h = *reinterpret_cast<const uint16_t*>(p + (int64_t)(at + e) * EB);
-#pragma unroll
-          for (int i = 0; i < WORDS; ++i)
-            if (i == e / 2) raw[i] = e & 1 ? (raw[i] & 0xffffu) | (h << 16) : (raw[i] & 0xffff0000u) | h;
-        }
+      uint16_t* half = reinterpret_cast<uint16_t*>(raw);
+      for (int e = 0; e < kElems; ++e) {        // token e - (kElems - vocab), as if there were more before it
+        const int64_t t = max(e - (kElems - a.vocab), 0);
+        if constexpr (EB == 4) raw[e] = *reinterpret_cast<const uint32_t*>(p + t * EB);
+        else half[e] = *reinterpret_cast<const uint16_t*>(p + t * EB);
       }
     }
   };
-  load(t0);
-  for (int base = t0; base < t1; base += kChunk) {
+  struct Sums {
+    double plain, far;
+    float ref;
+    bool bad;
+  };
+  auto chunk = [&](auto whole, int base, Sums u) -> Sums {   // (by value: references end up in memory)
+    constexpr bool kWhole = decltype(whole)::value;
     float x[kElems];
-    Logit<DT>::unpack(raw, x);
+    Logit<DT>::template unpack<kElems>(raw, x);
     if (base + kChunk < t1) load(base + kChunk);
-    float mx = x[0];
+    const int gone = min(base + (lane + 1) * kElems - t1, kElems);   // of a cut lane's logits the first so many are not its own
+    if constexpr (!kWhole) {
 #pragma unroll
-    for (int e = 1; e < kElems; ++e) mx = __builtin_elementwise_maximum(mx, x[e]);   // (NaN if one is)
-    bad |= !(mx < INFINITY);
-    // the reference moves up only where 2^t might leave fp64's range
-    if (__ballot(mx > ref + reach)) {
-      const float to = wave_max_f32(mx);
-      sum *= exp2_f64(fmax(((double)ref - (double)to) * cl, -1000.0));
-      ref = to;
+      for (int e = 0; e < kElems; ++e) x[e] = gone == kElems ? 0.f : e < gone ? x[kElems - 1] : x[e];
     }
-    if (ref > -INFINITY) {
+    float most = x[0], least = x[0];
 #pragma unroll
-      for (int e = 0; e < kElems; ++e) sum += exp2_f64(fmax(((double)x[e] - (double)ref) * cl, -1000.0));
+    for (int e = 1; e < kElems; ++e) {
+      most = __builtin_elementwise_maximum(most, x[e]);              // (NaN if one is)
+      least = __builtin_elementwise_minimum(least, x[e]);
     }
-    float m = mx;                               // lane 15 of 16 ends with the largest of them
-    m = fmaxf(m, __uint_as_float(dpp_u32<0x111>(__float_as_uint(m), __float_as_uint(m))));
-    m = fmaxf(m, __uint_as_float(dpp_u32<0x112>(__float_as_uint(m), __float_as_uint(m))));
-    m = fmaxf(m, __uint_as_float(dpp_u32<0x114>(__float_as_uint(m), __float_as_uint(m))));
-    m = fmaxf(m, __uint_as_float(dpp_u32<0x118>(__float_as_uint(m), __float_as_uint(m))));
+    u.bad |= !(most < INFINITY);
+    const bool plainly = __ballot(!(least > sc.low && most < sc.high)) == 0;
+    if constexpr (!kWhole) {
+      if (gone == kElems) most = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < kElems; ++e) x[e] = e < gone ? (plainly ? sc.absent : -INFINITY) : x[e];
+    }
+    if (__builtin_expect(plainly, 1)) {
+#pragma unroll
+      for (int e = 0; e < kElems; e += kTogether) u.plain = add_exp2_of_products<kTogether>(u.plain, x + e, sc.c);
+    } else {
+      // the reference moves up only where 2^t might leave fp64's range
+      if (__ballot(most > u.ref + reach)) {
+        const float to = wave_max_f32(most);
+        u.far *= exp2_f64(((double)u.ref - (double)to) * sc.c);
+        u.ref = to;
+      }
+      if (u.ref > -INFINITY) {
+#pragma unroll
+        for (int e = 0; e < kElems; ++e) u.far += exp2_f64(((double)x[e] - (double)u.ref) * sc.c);
+      }
+    }
+    uint32_t m = f32_key(most);                 // lane 15 of 16 ends with the largest of them
+    m = op_max(m, dpp_u32<0x111>(0u, m));
+    m = op_max(m, dpp_u32<0x112>(0u, m));
+    m = op_max(m, dpp_u32<0x114>(0u, m));
+    m = op_max(m, dpp_u32<0x118>(0u, m));
     const int block = (base - t0) / kBlock + lane / 16;
-    if (lane % 16 == 15 && block * kBlock < t1 - t0) peak[block] = m;
-  }
-  sum = wave_sum_f64_dpp(sum);
-  const bool any_bad = __ballot(bad) != 0;
-  if (lane == 0) a.parts[w] = BeamPart{sum, ref, any_bad};
+    if (lane % 16 == 15 && (kWhole || block * kBlock < t1 - t0)) peak[block] = m;
+    return u;
+  };
+  load(t0);
+  Sums u{0.0, 0.0, -INFINITY, false};
+  int base = t0;
+  for (; base + kChunk <= t1; base += kChunk) u = chunk(std::true_type(), base, u);
+  if (base < t1) u = chunk(std::false_type(), base, u);
+  u.far = wave_sum_f64_dpp(u.far);
+  u.plain = wave_sum_f64_dpp(u.plain);
+  const bool bad = __ballot(u.bad) != 0;
+  if (lane == 0) a.parts[w] = BeamPart{u.plain, u.far, u.ref, bad};
 }
 
 // ---- the n largest of many keys, by one wave ------------------------------------------------------------------------------
@@ -175,7 +241,7 @@ __device__ __forceinline__ uint64_t lane_bound(uint64_t mine, int n, SortRoom& r
   room.key[lane] = mine;
   wave_sync();
   int larger = 0;
-#pragma unroll 16
+#pragma unroll 4
   for (int j = 0; j < kWave; ++j) { const uint64_t k = room.key[j]; larger += k > mine || (k == mine && j < lane); }
   const uint64_t bound = room.key[__ffsll((unsigned long long)__ballot(larger == n - 1)) - 1];
   wave_sync();
@@ -194,7 +260,7 @@ __device__ __forceinline__ int sort_room(SortRoom& room, int c, int n, uint64_t*
   for (int i = lane; i < c; i += kWave) {
     const uint64_t k = room.key[i];
     int rank = 0;
-#pragma unroll 8
+#pragma unroll 4
     for (int j = 0; j < c; ++j) { const uint64_t o = room.key[j]; rank += o > k || (o == k && j < i); }
     if (rank < n) { keys[rank] = k; items[rank] = room.item[i]; }
   }
@@ -227,29 +293,19 @@ __device__ __forceinline__ int take_exactly(Key key, int n_items, int n, uint64_
   return c;
 }
 // the n largest of key(i), i < n_items, equals in order of items
-template <class K, class Key>
+template <int BITS, class Key>
 __device__ __forceinline__ int top_items(Key key, int n_items, int n, SortRoom& room, uint64_t* keys, uint32_t* items, int lane) {
-  constexpr int kHeld = 16;                               // keys of a lane at a time
-  K held[kHeld], mine = 0;
-  const int step = kHeld * kWave;
-  auto load = [&](int i0) {
-#pragma unroll
-    for (int e = 0; e < kHeld; ++e) { const int i = i0 + e * kWave + lane; held[e] = i < n_items ? key(i) : 0; }
-  };
-  for (int i0 = 0; i0 < n_items; i0 += step) {
-    load(i0);
-#pragma unroll
-    for (int e = 0; e < kHeld; ++e) mine = held[e] > mine ? held[e] : mine;
-  }
+  uint64_t mine = 0;
+#pragma unroll 4
+  for (int i = lane; i < n_items; i += kWave) { const uint64_t k = key(i); mine = k > mine ? k : mine; }
   const uint64_t bound = lane_bound(mine, n, room, lane);
   int c = 0;
-  for (int i0 = 0; i0 < n_items; i0 += step) {
-    if (n_items > step) load(i0);
-#pragma unroll
-    for (int e = 0; e < kHeld; ++e)
-      if (i0 + e * kWave < n_items) take(held[e], (uint32_t)(i0 + e * kWave + lane), held[e] >= bound, room, c, lane);
+#pragma unroll 4
+  for (int i0 = 0; i0 < n_items; i0 += kWave) {
+    const uint64_t k = i0 + lane < n_items ? key(i0 + lane) : 0;
+    take(k, (uint32_t)(i0 + lane), k >= bound, room, c, lane);
   }
-  if (c > kSortRoom) c = take_exactly<sizeof(K) * 8>(key, n_items, n, bound, room, lane);
+  if (__builtin_expect(c > kSortRoom, 0)) c = take_exactly<BITS>(key, n_items, n, bound, room, lane);
   return sort_room(room, c, n, keys, items, lane);
 }
 
@@ -267,14 +323,14 @@ struct JoinWave {
 
 template <int DT>
 __global__ __launch_bounds__(1024) void beam_join_kernel(BeamArgs a) {
-  constexpr int EB = Logit<DT>::bytes, WORDS = kElems * EB / 4, kAtOnce = kWave / 16;   // blocks that a wave reads at a time
+  constexpr int EB = Logit<DT>::bytes, kEach = 8, kLanes = kBlock / kEach, kAtOnce = kWave / kLanes;   // blocks are read two at a time
   extern __shared__ __align__(16) uint8_t lds[];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, waves = blockDim.x >> 6, group = blockIdx.x;
   JoinWave& mine = reinterpret_cast<JoinWave*>(lds)[wave];
   uint64_t* rank = reinterpret_cast<uint64_t*>(lds + waves * sizeof(JoinWave));    // [beams, n] keys of the ranks, 0: none
   uint2* cand = reinterpret_cast<uint2*>(rank + a.beams * a.n);                    // [beams, n]
   RowOffer* offer = reinterpret_cast<RowOffer*>(cand + a.beams * a.n);             // [beams]
-  const double cl = a.scale * kLog2e;
+  const double c_log2 = a.scale * kLog2e;
   for (int b = wave; b < a.beams; b += waves) {
     const int row = group * a.beams + b;
     const float s = a.scores[row];
@@ -287,17 +343,26 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(BeamArgs a) {
       if (lane == 0) cand[b * a.n] = make_uint2(0u, (uint32_t)a.end_token);
     } else if (row_lives(s)) {
       const BeamPart* parts = a.parts + (int64_t)row * a.n_parts;
-      bool bad = false;
+      bool bad = false, plain = false;
       float ref = -INFINITY;
-      for (int i = lane; i < a.n_parts; i += kWave) { bad |= parts[i].bad != 0; ref = fmaxf(ref, parts[i].ref); }
+      for (int i = lane; i < a.n_parts; i += kWave) {
+        const BeamPart q = parts[i];
+        bad |= q.bad != 0;
+        plain |= q.plain > 0.0;
+        ref = fmaxf(ref, q.ref);
+      }
       ref = wave_max_f32(ref);
+      if (__ballot(plain)) ref = fmaxf(ref, 0.f);       // (plain sums are relative to a logit of 0)
       if (!__ballot(bad) && ref > -INFINITY) {
-        const float* peak = a.peaks + (int64_t)row * a.n_blocks;
-        const int n_best = top_items<uint32_t>([&](int i) { const float x = peak[i]; return x > -INFINITY ? f32_key(x) : 0u; }, a.n_blocks, a.n,
+        const uint32_t* peak = a.peaks + (int64_t)row * a.n_blocks;
+        const int n_best = top_items<32>([&](int i) -> uint64_t { const uint32_t k = peak[i]; return k > kLowestKey ? k : 0u; }, a.n_blocks, a.n,
                                          mine.room, mine.keys, mine.items, lane);
         double sum = 0.0;
-        for (int i = lane; i < a.n_parts; i += kWave)
-          if (parts[i].ref > -INFINITY) sum += parts[i].sum * exp2_f64(fmax(((double)parts[i].ref - (double)ref) * cl, -1000.0));
+        for (int i = lane; i < a.n_parts; i += kWave) {
+          const BeamPart q = parts[i];
+          sum += q.plain * exp2_f64(-(double)ref * c_log2);
+          if (q.ref > -INFINITY) sum += q.sum * exp2_f64(((double)q.ref - (double)ref) * c_log2);
+        }
         sum = wave_sum_f64_dpp(sum);
         o.base = (double)s - log(sum);
         o.ref = ref;
@@ -306,19 +371,19 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(BeamArgs a) {
         auto key_of = [&](float x, int t) { return x > -INFINITY ? ((uint64_t)f32_key(x) << 32) | (uint32_t)~t : 0ull; };
         auto each_token = [&](auto f) {
           for (int i0 = 0; i0 < n_best; i0 += kAtOnce) {
-            const int i = i0 + lane / 16;
-            const int at = i < n_best ? (int)mine.items[i] * kBlock + lane % 16 * kElems : a.vocab;
-            float x[kElems];
-            if (at + kElems <= a.vocab) {
-              uint32_t raw[WORDS];
-              __builtin_memcpy(raw, p + (int64_t)at * EB, kElems * EB);
-              Logit<DT>::unpack(raw, x);
+            const int i = i0 + lane / kLanes;
+            const int at = i < n_best ? (int)mine.items[i] * kBlock + lane % kLanes * kEach : a.vocab;
+            float x[kEach];
+            if (at + kEach <= a.vocab) {
+              uint32_t raw[kEach * EB / 4];
+              __builtin_memcpy(raw, p + (int64_t)at * EB, kEach * EB);
+              Logit<DT>::template unpack<kEach>(raw, x);
             } else {
 #pragma unroll
-              for (int e = 0; e < kElems; ++e) x[e] = at + e < a.vocab ? Logit<DT>::one(p + (int64_t)(at + e) * EB) : -INFINITY;
+              for (int e = 0; e < kEach; ++e) x[e] = at + e < a.vocab ? Logit<DT>::one(p + (int64_t)(at + e) * EB) : -INFINITY;
             }
 #pragma unroll
-            for (int e = 0; e < kElems; ++e) f(key_of(x[e], at + e));
+            for (int e = 0; e < kEach; ++e) f(key_of(x[e], at + e));
           }
         };
         uint64_t bound;
@@ -331,7 +396,7 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(BeamArgs a) {
         }
         int c = 0;
         each_token([&](uint64_t k) { if (__ballot(k >= bound)) take(k, 0, k >= bound, mine.room, c, lane); });
-        if (c > kSortRoom)
+        if (__builtin_expect(c > kSortRoom, 0))
           c = take_exactly<64>([&](int i) -> uint64_t {
             const int t = (int)mine.items[i / kBlock] * kBlock + i % kBlock;
             return t < a.vocab ? key_of(Logit<DT>::one(p + (int64_t)t * EB), t) : 0;
@@ -347,7 +412,7 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(BeamArgs a) {
   __syncthreads();
   if (wave) return;
   // of all rows' candidates, in order of rows and places
-  const int count = top_items<uint64_t>([&](int i) { return rank[i]; }, a.beams * a.n, a.n, mine.room, mine.keys, mine.items, lane);
+  const int count = top_items<64>([&](int i) { return rank[i]; }, a.beams * a.n, a.n, mine.room, mine.keys, mine.items, lane);
   // (all that this group's rows held has been read before anything is written: the outputs may be the inputs)
   float out_s = -INFINITY;
   int parent = -1, token = -1, length = 0;
@@ -390,10 +455,11 @@ hipError_t launch(const BeamArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// Tokens of a part: as many chunks as leave 8192 waves, a third more than the chip holds.  (32 x 16 rows of 256K bf16, 8 / 16 / 32 chunks: 93.3 / 93.4 /
+// 99.8 us.)
 int beam_part_len(int64_t rows, int vocab) {
-  const int64_t all = rows * (((int64_t)vocab + kChunk - 1) / kChunk);   // chunks
-  const int64_t per = (all + 8191) / 8192;
-  return (int)(per < 1 ? 1 : per > 1024 ? 1024 : per) * kChunk;
+  const int64_t per = (rows * (((int64_t)vocab + kChunk - 1) / kChunk) + 8191) / 8192;
+  return (int)std::min<int64_t>(std::max<int64_t>(per, 1), 1024) * kChunk;
 }
 int beam_blocks(int vocab) { return (int)(((int64_t)vocab + kBlock - 1) / kBlock); }
 

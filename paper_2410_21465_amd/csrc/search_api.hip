@@ -51,7 +51,7 @@ BeamLayout beam_layout(const shadowkv_logits* x) {
   L.n_parts = (int)(((int64_t)x->vocab + L.part_len - 1) / L.part_len);
   L.n_blocks = beam_blocks(x->vocab);
   L.peaks = up((size_t)rows * L.n_parts * sizeof(BeamPart));
-  L.total = std::max(L.peaks + up((size_t)rows * L.n_blocks * sizeof(float)), kAlign);
+  L.total = std::max(L.peaks + up((size_t)rows * L.n_blocks * sizeof(uint32_t)), kAlign);
   return L;
 }
 
@@ -125,7 +125,7 @@ int shadowkv_beam_select(const shadowkv_logits* logits, const float* scores, con
   a.out_scores = out_scores; a.out_parents = out_parents; a.out_tokens = out_tokens; a.out_finished = out_finished; a.out_lengths = out_lengths;
   a.parts = static_cast<BeamPart*>(workspace);
   a.n_blocks = L.n_blocks;
-  a.peaks = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.peaks);
+  a.peaks = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + L.peaks);
   const hipError_t e = launch_beam_select(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SHADOWKV_OK : fail_hip("beam select", e);
 }
