@@ -264,6 +264,18 @@ struct BeamPart {           // of a row: sums over a part of exp(c x), and of ex
   float ref;                // -inf: no such logit above minus infinity
   int bad;                  // a logit is NaN or plus infinity
 };
+struct BeamRange {          // of logits that are summed as they are
+  double c;                 // logit_scale in units of log 2
+  float low, high;          // x between them
+  float absent;             // adds 2^-900: what stands behind the last token
+  float reach;              // others move their reference by more than this
+};
+BeamRange beam_range(double scale);
+struct BeamOffer {          // what a row offers
+  uint64_t rank;            // key of its rank; 0: nothing
+  float score;
+  int32_t token;
+};
 struct BeamArgs {
   const uint8_t* logits;    // strides in bytes
   int64_t group_stride, beam_stride;
@@ -271,6 +283,7 @@ struct BeamArgs {
   int part_len, n_parts;    // tokens of a part (a multiple of 1024), parts of a row
   int n_blocks;             // blocks of 256 tokens of a row
   double scale, penalty;
+  BeamRange range;
   const float* scores;
   const uint8_t* finished;
   const int32_t* lengths;
@@ -281,6 +294,7 @@ struct BeamArgs {
   int32_t* out_lengths;
   BeamPart* parts;          // [rows, n_parts]
   uint32_t* peaks;          // [rows, n_blocks] largest logit of a block, as a key
+  BeamOffer* offers;        // [rows, n]
 };
 int beam_part_len(int64_t rows, int vocab);
 int beam_blocks(int vocab);

@@ -1,9 +1,11 @@
 // The n best continuations of every group of beams, by summed log-probability:
 //   score = s + c x_v - log sum_w exp(c x_w),   rank = score / length^a.
-// Two launches.  The first reads the logits once: a wave takes a part of a row, sums its exponentials (fp64) and keeps the largest logit of
-// every block of 256 tokens, nothing else.  The second has a workgroup per group and a wave per row: the
-// n best tokens of a row lie in the n blocks with the largest maxima (whatever lies in another block has n better ones, one in each of
-// those), so it finds these, reads them again, and keeps their n best; then the first wave ranks what all rows offer.
+// Three launches.  The first reads the logits once: a wave takes a part of a row, sums its exponentials (fp64) and keeps the largest logit of
+// every block of 256 tokens, nothing else.  The second has a workgroup per row.  The n best tokens of a row lie in the n blocks with the
+// largest maxima (whatever lies in another block has n better ones, one in each of those), so it finds these, reads them again, and
+// keeps their n best.  The third, a workgroup per group, ranks what all rows offer.  (Done by the group's last workgroup of the second launch instead,
+// behind a counter, the choice costs more than its launch: every workgroup has to write its L2 back first.  32 x 16 rows: 82 us for
+// both.)
 //
 // Ranks of different rows meet in the choice, so the sums are fp64: exp as 2^t = 2^round(t) 2^f, f in [-1/2, 1/2], with 2^f the Chebyshev
 // interpolation of degree 8 (off by 1.1e-12 at most), 2^round(t) added to the exponent's bits.  Lanes take the same tokens in the same
@@ -116,34 +118,17 @@ __device__ __forceinline__ bool row_lives(float score) { return fabsf(score) < I
 
 // Logits x with -800 < x c < 900 (c in units of log 2) are summed as they are, 2^(x c); a chunk with others (masks, infinities, logits far apart)
 // is summed relative to a logit that it or an earlier one holds, in a sum of its own.
-struct BeamScale {
-  double c;
-  float low, high;                              // x between them
-  float absent;                                 // adds 2^-900: what stands behind the last token
-};
-__device__ __forceinline__ BeamScale beam_scale(double scale) {
-  BeamScale s;
-  s.c = scale * kLog2e;
-  const bool fits = s.c > 0x1p-60 && s.c < 0x1p60;   // (else the borders leave fp32's range)
-  s.low = fits ? (float)(-800.0 / s.c) : INFINITY;
-  s.high = fits ? (float)(900.0 / s.c) : -INFINITY;
-  s.absent = fits ? (float)(-900.0 / s.c) : -INFINITY;
-  return s;
-}
-
 template <int DT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6, 6))) void beam_parts_kernel(BeamArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(5, 5))) void beam_parts_kernel(BeamArgs a) {
   constexpr int EB = Logit<DT>::bytes, WORDS = kElems * EB / 4;
   const int lane = threadIdx.x & (kWave - 1);
   const uint32_t w = blockIdx.x * 4 + (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   if (w >= (uint32_t)(a.groups * a.beams) * (uint32_t)a.n_parts) return;
   const int row = (int)(w / (uint32_t)a.n_parts), part = (int)(w % (uint32_t)a.n_parts);
-  if (!row_lives(a.scores[row]) || (a.finished && a.finished[row])) return;   // (the second launch asks the same)
   const uint8_t* p = a.logits + (row / a.beams) * a.group_stride + (row % a.beams) * a.beam_stride;
   const int t0 = part * a.part_len, t1 = min(a.vocab, t0 + a.part_len);
   uint32_t* peak = a.peaks + (int64_t)row * a.n_blocks + t0 / kBlock;
-  const BeamScale sc = beam_scale(a.scale);
-  const float reach = (float)fmin(500.0 / sc.c, 1e38);
+  const BeamRange sc = a.range;
   uint32_t raw[WORDS];
   // rows of an odd vocabulary begin at any element; a lane that the end cuts off reads the last kElems tokens
   auto load = [&](int base) {
@@ -192,7 +177,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6, 6))) voi
       for (int e = 0; e < kElems; e += kTogether) u.plain = add_exp2_of_products<kTogether>(u.plain, x + e, sc.c);
     } else {
       // the reference moves up only where 2^t might leave fp64's range
-      if (__ballot(most > u.ref + reach)) {
+      if (__ballot(most > u.ref + sc.reach)) {
         const float to = wave_max_f32(most);
         u.far *= exp2_f64(((double)u.ref - (double)to) * sc.c);
         u.ref = to;
@@ -211,7 +196,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6, 6))) voi
     if (lane % 16 == 15 && (kWhole || block * kBlock < t1 - t0)) peak[block] = m;
     return u;
   };
-  load(t0);
+  load(t0);                                     // (on its way while it turns out whether the row takes part; the second launch asks the same)
+  if (!row_lives(a.scores[row]) || (a.finished && a.finished[row])) return;
   Sums u{0.0, 0.0, -INFINITY, false};
   int base = t0;
   for (; base + kChunk <= t1; base += kChunk) u = chunk(std::true_type(), base, u);
@@ -222,126 +208,165 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6, 6))) voi
   if (lane == 0) a.parts[w] = BeamPart{u.plain, u.far, u.ref, bad};
 }
 
-// ---- the n largest of many keys, by one wave ------------------------------------------------------------------------------
-// What reaches a bound that n keys reach, and few others do, is put into LDS in order of items and sorted by counting, for each, what is
-// larger (the earlier of equals first).
-constexpr int kSortRoom = 256;
-struct SortRoom {
-  uint64_t key[kSortRoom];
-  uint32_t item[kSortRoom];
+// ---- the n largest of many keys, by a workgroup --------------------------------------------------------------------------
+// What reaches a bound that n keys reach, and few others do, is put into LDS and sorted by counting, for each, what is larger.  Keys are 64 bits
+// wide, 0 is none; they come with a number, and of equal keys the lower number goes first (kTies; other keys are never equal).
+constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / kWave;
+struct __align__(16) JoinRoom {
+  uint64_t key[kJoinThreads];
+  uint32_t item[kJoinThreads];
+  uint32_t upper[kJoinThreads];
+  uint64_t best[64];                                      // what comes out, in order
+  uint32_t best_item[64];
+  uint32_t bound;
+  int count, other;
 };
-// between writes and reads of LDS by different lanes of a wave
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-// the n-th largest of the lanes' keys (1 if that is 0, no key)
-__device__ __forceinline__ uint64_t lane_bound(uint64_t mine, int n, SortRoom& room, int lane) {
-  room.key[lane] = mine;
-  wave_sync();
-  int larger = 0;
-#pragma unroll 4
-  for (int j = 0; j < kWave; ++j) { const uint64_t k = room.key[j]; larger += k > mine || (k == mine && j < lane); }
-  const uint64_t bound = room.key[__ffsll((unsigned long long)__ballot(larger == n - 1)) - 1];
-  wave_sync();
-  return bound ? bound : 1;
-}
-// c: keys that have been taken, counted beyond the room as well
-__device__ __forceinline__ void take(uint64_t k, uint32_t item, bool takes, SortRoom& room, int& c, int lane) {
+__device__ __forceinline__ void take(uint64_t k, uint32_t item, bool takes, JoinRoom& room, int lane) {
   const uint64_t taken = __ballot(takes);
-  const int at = c + __popcll(taken & ((1ull << lane) - 1));
-  if (takes && at < kSortRoom) { room.key[at] = k; room.item[at] = item; }
-  c += __popcll(taken);
+  if (taken == 0) return;
+  int at = 0;
+  if (lane == 0) at = atomicAdd(&room.count, __popcll(taken));
+  at = __builtin_amdgcn_readfirstlane(at) + __popcll(taken & ((1ull << lane) - 1));
+  if (takes && at < kJoinThreads) { room.key[at] = k; room.item[at] = item; }
 }
-// the n best of the c <= kSortRoom in the room, in order; returns how many there are
-__device__ __forceinline__ int sort_room(SortRoom& room, int c, int n, uint64_t* keys, uint32_t* items, int lane) {
-  wave_sync();
-  for (int i = lane; i < c; i += kWave) {
-    const uint64_t k = room.key[i];
+// what is in the room, in order; all threads, after a barrier
+template <bool kTies>
+__device__ __forceinline__ int sort_room(JoinRoom& room, int n, int tid) {
+  const int c = room.count;
+  if (tid >= c && tid < ((c + 7) & ~7)) { room.key[tid] = 0; room.item[tid] = ~0u; }
+  __syncthreads();
+  if (tid < c) {
+    const uint64_t k = room.key[tid];
+    const uint32_t item = room.item[tid];
     int rank = 0;
-#pragma unroll 4
-    for (int j = 0; j < c; ++j) { const uint64_t o = room.key[j]; rank += o > k || (o == k && j < i); }
-    if (rank < n) { keys[rank] = k; items[rank] = room.item[i]; }
+    for (int j = 0; j < c; j += 8) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&room.key[j + e]);
+        rank += o.x > k;
+        rank += o.y > k;
+        if constexpr (kTies) {
+          rank += o.x == k && room.item[j + e] < item;
+          rank += o.y == k && room.item[j + e + 1] < item;
+        }
+      }
+    }
+    if (rank < n) { room.best[rank] = k; room.best_item[rank] = item; }
   }
-  wave_sync();
+  __syncthreads();
   return min(c, n);
 }
-// Where more than the room reach a bound (many equal keys, say): the largest bound that n keys reach, bit by bit, and of the
-// keys that equal it the first.  key(i): of item i < n_items, 0: none.
-template <int BITS, class Key>
-__device__ __forceinline__ int take_exactly(Key key, int n_items, int n, uint64_t bound, SortRoom& room, int lane) {
-  auto count = [&](uint64_t from) {
+// A key that n keys reach, from the upper halves (at least 1: a key of 0 is none): the n-th largest of the threads' own largest, or up to kFewPlaces
+// places, which 64 values are enough for, of the largest of four threads.
+constexpr int kFewPlaces = 16;
+__device__ __forceinline__ uint64_t find_bound(uint64_t largest, int n, JoinRoom& room, int tid) {
+  const int lane = tid & (kWave - 1);
+  uint32_t mine = (uint32_t)(largest >> 32), bound;
+  room.upper[tid] = mine;
+  if (tid == 0) { room.count = 0; room.bound = ~0u; }
+  __syncthreads();
+  int larger = 0;
+  if (n <= kFewPlaces) {                                  // (every wave finds it by itself)
+    mine = room.upper[lane];
+#pragma unroll
+    for (int v = 1; v < kJoinWaves; ++v) mine = op_max(mine, room.upper[v * kWave + lane]);
+#pragma unroll 8
+    for (int j = 0; j < kWave; ++j) larger += (uint32_t)__builtin_amdgcn_readlane((int)mine, j) > mine;
+    bound = wave_min_u32(larger < n ? mine : ~0u);
+  } else {
+#pragma unroll 4
+    for (int j = 0; j < kJoinThreads; j += 4) {
+      const uint4 o = *reinterpret_cast<const uint4*>(&room.upper[j]);
+      larger += o.x > mine;
+      larger += o.y > mine;
+      larger += o.z > mine;
+      larger += o.w > mine;
+    }
+    const uint32_t least = wave_min_u32(larger < n ? mine : ~0u);
+    if (lane == 0) atomicMin(&room.bound, least);
+    __syncthreads();
+    bound = room.bound;
+  }
+  return bound ? (uint64_t)bound << 32 : 1;
+}
+// Where more reach the bound than there is room for (many equal ones, say): the largest bound that n keys reach, bit by bit, and of the keys that
+// equal it the lowest numbers.  key(i, item): of entry i < n_entries, and its number.
+template <bool kTies, class Key>
+__device__ __forceinline__ void take_exactly(Key key, int n_entries, int n, uint64_t bound, JoinRoom& room, int tid) {
+  const int lane = tid & (kWave - 1);
+  // how many are above `from`, or equal it and have a number below `below`
+  auto count = [&](uint64_t from, uint32_t below) {
+    __syncthreads();
+    if (tid == 0) room.other = 0;
+    __syncthreads();
     int c = 0;
-    for (int i0 = 0; i0 < n_items; i0 += kWave) c += __popcll(__ballot(i0 + lane < n_items && key(i0 + lane) >= from));
-    return c;
+    for (int i = tid; i < n_entries; i += kJoinThreads) {
+      uint32_t item = 0;
+      const uint64_t k = key(i, item);
+      c += k > from || (k == from && item < below);
+    }
+    if (c) atomicAdd(&room.other, c);
+    __syncthreads();
+    return room.other;
   };
-  for (int b = BITS - 1; b >= 0; --b) {
+  for (int b = 63; b >= 0; --b) {
     const uint64_t up = (bound >> b | 1ull) << b;         // (bits above b are right; where bit b is set already this is not more)
-    const int reach = up > bound ? count(up) : 0;
-    if (reach >= n) bound = up;
-    if (reach == n) break;
+    if (up > bound && count(up - 1, 0) >= n) bound = up;
   }
-  const int spare = n - count(bound + 1);
-  int c = 0, equal = 0;
-  wave_sync();
-  for (int i0 = 0; i0 < n_items; i0 += kWave) {
-    const uint64_t k = i0 + lane < n_items ? key(i0 + lane) : 0, same = __ballot(k == bound);
-    take(k, (uint32_t)(i0 + lane), k > bound || (k == bound && equal + __popcll(same & ((1ull << lane) - 1)) < spare), room, c, lane);
-    equal += __popcll(same);
+  uint32_t below = ~0u;
+  if constexpr (kTies) {                                  // the most numbers that do not make n yet, and one more
+    below = 0;
+    for (int b = 31; b >= 0; --b)
+      if (count(bound, below | 1u << b) < n) below |= 1u << b;
+    ++below;
   }
-  return c;
+  if (tid == 0) room.count = 0;
+  __syncthreads();
+  for (int i0 = 0; i0 < n_entries; i0 += kJoinThreads) {
+    uint32_t item = 0;
+    const uint64_t k = i0 + tid < n_entries ? key(i0 + tid, item) : 0;
+    take(k, item, k > bound || (k == bound && item < below), room, lane);
+  }
+  __syncthreads();
 }
-// the n largest of key(i), i < n_items, equals in order of items
-template <int BITS, class Key>
-__device__ __forceinline__ int top_items(Key key, int n_items, int n, SortRoom& room, uint64_t* keys, uint32_t* items, int lane) {
+template <bool kTies, class Key>
+__device__ __forceinline__ int top_items(Key key, int n_entries, int n, JoinRoom& room, int tid) {
+  const int lane = tid & (kWave - 1);
   uint64_t mine = 0;
+  uint32_t item = 0;
 #pragma unroll 4
-  for (int i = lane; i < n_items; i += kWave) { const uint64_t k = key(i); mine = k > mine ? k : mine; }
-  const uint64_t bound = lane_bound(mine, n, room, lane);
-  int c = 0;
+  for (int i = tid; i < n_entries; i += kJoinThreads) { const uint64_t k = key(i, item); mine = k > mine ? k : mine; }
+  const uint64_t bound = find_bound(mine, n, room, tid);
 #pragma unroll 4
-  for (int i0 = 0; i0 < n_items; i0 += kWave) {
-    const uint64_t k = i0 + lane < n_items ? key(i0 + lane) : 0;
-    take(k, (uint32_t)(i0 + lane), k >= bound, room, c, lane);
+  for (int i0 = 0; i0 < n_entries; i0 += kJoinThreads) {
+    const uint64_t k = i0 + tid < n_entries ? key(i0 + tid, item) : 0;
+    take(k, item, k >= bound, room, lane);
   }
-  if (__builtin_expect(c > kSortRoom, 0)) c = take_exactly<BITS>(key, n_items, n, bound, room, lane);
-  return sort_room(room, c, n, keys, items, lane);
+  __syncthreads();
+  if (__builtin_expect(room.count > kJoinThreads, 0)) take_exactly<kTies>(key, n_entries, n, bound, room, tid);
+  return sort_room<kTies>(room, n, tid);
 }
-
-// What a row offers: candidate i is (logit, token); score = base + c (logit - ref).
-struct RowOffer {
-  double base;
-  float ref;
-  int count;
-};
-struct JoinWave {
-  SortRoom room;
-  uint64_t keys[64];
-  uint32_t items[64];
-};
 
 template <int DT>
-__global__ __launch_bounds__(1024) void beam_join_kernel(BeamArgs a) {
-  constexpr int EB = Logit<DT>::bytes, kEach = 8, kLanes = kBlock / kEach, kAtOnce = kWave / kLanes;   // blocks are read two at a time
-  extern __shared__ __align__(16) uint8_t lds[];
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, waves = blockDim.x >> 6, group = blockIdx.x;
-  JoinWave& mine = reinterpret_cast<JoinWave*>(lds)[wave];
-  uint64_t* rank = reinterpret_cast<uint64_t*>(lds + waves * sizeof(JoinWave));    // [beams, n] keys of the ranks, 0: none
-  uint2* cand = reinterpret_cast<uint2*>(rank + a.beams * a.n);                    // [beams, n]
-  RowOffer* offer = reinterpret_cast<RowOffer*>(cand + a.beams * a.n);             // [beams]
-  const double c_log2 = a.scale * kLog2e;
-  for (int b = wave; b < a.beams; b += waves) {
-    const int row = group * a.beams + b;
-    const float s = a.scores[row];
-    const bool done = a.finished && a.finished[row];
-    double weight = 1.0;
-    if (a.penalty != 0.0) weight = pow(fmax((double)a.lengths[row] + (done ? 0.0 : 1.0), 1.0), a.penalty);
-    RowOffer o{(double)s, 0.f, 0};
-    if (row_lives(s) && done) {
-      o.count = 1;
-      if (lane == 0) cand[b * a.n] = make_uint2(0u, (uint32_t)a.end_token);
-    } else if (row_lives(s)) {
+__global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
+  constexpr int EB = Logit<DT>::bytes, kEach = 8, kLanes = kBlock / kEach, kAtOnce = kJoinThreads / kLanes;
+  __shared__ JoinRoom room;
+  __shared__ double base_shared;
+  __shared__ float ref_shared;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, row = blockIdx.x, group = row / a.beams;
+  const double c_log2 = a.range.c;
+  const float s = a.scores[row];
+  const bool lives = row_lives(s), done = a.finished && a.finished[row];
+  double weight = 1.0;
+  if (a.penalty != 0.0) weight = pow(fmax((double)a.lengths[row] + (done ? 0.0 : 1.0), 1.0), a.penalty);
+  BeamOffer* offer = a.offers + (int64_t)row * a.n;
+  int count = 0;
+  if (lives && done) {
+    count = 1;
+    if (tid == 0) offer[0] = BeamOffer{f64_key((double)s / weight), s, a.end_token};
+  } else if (lives) {
+    // the row's sum, by one wave, while the others go ahead
+    if (wave == kJoinWaves - 1) {
       const BeamPart* parts = a.parts + (int64_t)row * a.n_parts;
       bool bad = false, plain = false;
       float ref = -INFINITY;
@@ -352,83 +377,97 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(BeamArgs a) {
         ref = fmaxf(ref, q.ref);
       }
       ref = wave_max_f32(ref);
-      if (__ballot(plain)) ref = fmaxf(ref, 0.f);       // (plain sums are relative to a logit of 0)
+      if (__ballot(plain)) ref = fmaxf(ref, 0.f);         // (plain sums are relative to a logit of 0)
+      double sum = 0.0;
       if (!__ballot(bad) && ref > -INFINITY) {
-        const uint32_t* peak = a.peaks + (int64_t)row * a.n_blocks;
-        const int n_best = top_items<32>([&](int i) -> uint64_t { const uint32_t k = peak[i]; return k > kLowestKey ? k : 0u; }, a.n_blocks, a.n,
-                                         mine.room, mine.keys, mine.items, lane);
-        double sum = 0.0;
         for (int i = lane; i < a.n_parts; i += kWave) {
           const BeamPart q = parts[i];
           sum += q.plain * exp2_f64(-(double)ref * c_log2);
           if (q.ref > -INFINITY) sum += q.sum * exp2_f64(((double)q.ref - (double)ref) * c_log2);
         }
         sum = wave_sum_f64_dpp(sum);
-        o.base = (double)s - log(sum);
-        o.ref = ref;
-        // tokens of those blocks that are not less than the n-th block's largest (of fewer blocks: than the n-th lane's)
-        const uint8_t* p = a.logits + group * a.group_stride + b * a.beam_stride;
-        auto key_of = [&](float x, int t) { return x > -INFINITY ? ((uint64_t)f32_key(x) << 32) | (uint32_t)~t : 0ull; };
-        auto each_token = [&](auto f) {
-          for (int i0 = 0; i0 < n_best; i0 += kAtOnce) {
-            const int i = i0 + lane / kLanes;
-            const int at = i < n_best ? (int)mine.items[i] * kBlock + lane % kLanes * kEach : a.vocab;
-            float x[kEach];
-            if (at + kEach <= a.vocab) {
-              uint32_t raw[kEach * EB / 4];
-              __builtin_memcpy(raw, p + (int64_t)at * EB, kEach * EB);
-              Logit<DT>::template unpack<kEach>(raw, x);
-            } else {
-#pragma unroll
-              for (int e = 0; e < kEach; ++e) x[e] = at + e < a.vocab ? Logit<DT>::one(p + (int64_t)(at + e) * EB) : -INFINITY;
-            }
-#pragma unroll
-            for (int e = 0; e < kEach; ++e) f(key_of(x[e], at + e));
-          }
-        };
-        uint64_t bound;
-        if (n_best == a.n) {
-          bound = mine.keys[n_best - 1] << 32;
-        } else {
-          uint64_t best = 0;
-          each_token([&](uint64_t k) { best = k > best ? k : best; });
-          bound = lane_bound(best, a.n, mine.room, lane);
-        }
-        int c = 0;
-        each_token([&](uint64_t k) { if (__ballot(k >= bound)) take(k, 0, k >= bound, mine.room, c, lane); });
-        if (__builtin_expect(c > kSortRoom, 0))
-          c = take_exactly<64>([&](int i) -> uint64_t {
-            const int t = (int)mine.items[i / kBlock] * kBlock + i % kBlock;
-            return t < a.vocab ? key_of(Logit<DT>::one(p + (int64_t)t * EB), t) : 0;
-          }, n_best * kBlock, a.n, bound, mine.room, lane);
-        o.count = sort_room(mine.room, c, a.n, mine.keys, mine.items, lane);
-        if (lane < o.count) cand[b * a.n + lane] = make_uint2(__float_as_uint(key_f32((uint32_t)(mine.keys[lane] >> 32))), ~(uint32_t)mine.keys[lane]);
+      } else {
+        ref = -INFINITY;                                  // nothing is offered
+      }
+      if (lane == 0) {
+        base_shared = (double)s - log(sum);
+        ref_shared = ref;
       }
     }
-    wave_sync();
-    if (lane == 0) offer[b] = o;
-    if (lane < a.n) rank[b * a.n + lane] = lane < o.count ? f64_key((o.base + a.scale * ((double)__uint_as_float(cand[b * a.n + lane].x) - (double)o.ref)) / weight) : 0;
+    const uint8_t* p = a.logits + (int64_t)group * a.group_stride + (int64_t)(row % a.beams) * a.beam_stride;
+    // (logit, ~number): among equal logits the lower token or block goes first
+    auto key_of = [](uint32_t upper, int number) -> uint64_t { return upper > kLowestKey ? ((uint64_t)upper << 32) | (uint32_t)~number : 0; };
+    auto token_key = [&](int t, uint32_t&) { return key_of(f32_key(Logit<DT>::one(p + (int64_t)t * EB)), t); };
+    if (a.n_blocks <= a.n) {                              // all blocks are among the n best
+      count = top_items<false>(token_key, a.vocab, a.n, room, tid);
+    } else {
+      const uint32_t* peak = a.peaks + (int64_t)row * a.n_blocks;
+      const int n_best = top_items<false>([&](int i, uint32_t&) { return key_of(peak[i], i); }, a.n_blocks, a.n, room, tid);
+      auto block = [&](int i) { return (int)~(uint32_t)room.best[i]; };
+      // tokens of those blocks that are not less than the n-th block's largest
+      const uint64_t bound = n_best == a.n ? room.best[n_best - 1] >> 32 << 32 : 1;
+      if (tid == 0) room.count = 0;
+      __syncthreads();
+      for (int i0 = 0; i0 < n_best; i0 += kAtOnce) {
+        const int i = i0 + tid / kLanes;
+        const int at = i < n_best ? block(i) * kBlock + tid % kLanes * kEach : a.vocab;
+        float x[kEach];
+        if (at + kEach <= a.vocab) {
+          uint32_t raw[kEach * EB / 4];
+          __builtin_memcpy(raw, p + (int64_t)at * EB, kEach * EB);
+          Logit<DT>::template unpack<kEach>(raw, x);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) x[e] = at + e < a.vocab ? Logit<DT>::one(p + (int64_t)(at + e) * EB) : -INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const uint64_t k = key_of(f32_key(x[e]), at + e);
+          take(k, 0, k >= bound, room, lane);
+        }
+      }
+      __syncthreads();
+      if (__builtin_expect(room.count > kJoinThreads, 0))
+        take_exactly<false>([&](int i, uint32_t& item) -> uint64_t {
+          const int t = block(i / kBlock) * kBlock + i % kBlock;
+          return t < a.vocab ? token_key(t, item) : 0;
+        }, n_best * kBlock, a.n, bound, room, tid);
+      count = sort_room<false>(room, a.n, tid);
+    }
+    if (ref_shared == -INFINITY) count = 0;
+    if (tid < count) {
+      const double score = base_shared + a.scale * ((double)key_f32((uint32_t)(room.best[tid] >> 32)) - (double)ref_shared);
+      offer[tid] = BeamOffer{f64_key(score / weight), (float)score, (int32_t)~(uint32_t)room.best[tid]};
+    }
   }
-  __syncthreads();
-  if (wave) return;
-  // of all rows' candidates, in order of rows and places
-  const int count = top_items<64>([&](int i) { return rank[i]; }, a.beams * a.n, a.n, mine.room, mine.keys, mine.items, lane);
+  if (tid >= count && tid < a.n) offer[tid] = BeamOffer{0, -INFINITY, -1};
+}
+
+__global__ __launch_bounds__(kJoinThreads) void beam_choose_kernel(BeamArgs a) {
+  __shared__ JoinRoom room;
+  const int tid = threadIdx.x, group = blockIdx.x;
+  const BeamOffer* all = a.offers + (int64_t)group * a.beams * a.n;
+  const int found = top_items<true>([&](int i, uint32_t& item) -> uint64_t {
+    item = (uint32_t)i;                                   // in order of rows, then of places
+    return all[i].rank;
+  }, a.beams * a.n, a.n, room, tid);
   // (all that this group's rows held has been read before anything is written: the outputs may be the inputs)
   float out_s = -INFINITY;
   int parent = -1, token = -1, length = 0;
   bool ended = false;
-  if (lane < count) {
-    const int i = (int)mine.items[lane], b = i / a.n, row = group * a.beams + b;
-    const bool was = a.finished && a.finished[row];
-    out_s = (float)(offer[b].base + a.scale * ((double)__uint_as_float(cand[i].x) - (double)offer[b].ref));
-    parent = row;
-    token = (int)cand[i].y;
+  if (tid < found) {
+    const int i = (int)room.best_item[tid];
+    const BeamOffer o = all[i];
+    parent = group * a.beams + i / a.n;
+    const bool was = a.finished && a.finished[parent];
+    out_s = o.score;
+    token = o.token;
     ended = was || (a.end_token >= 0 && token == a.end_token);
-    if (a.out_lengths) length = a.lengths[row] + (was ? 0 : 1);
+    if (a.out_lengths) length = a.lengths[parent] + (was ? 0 : 1);
   }
   __builtin_amdgcn_s_waitcnt(0);
-  if (lane < a.n) {
-    const int at = group * a.n + lane;
+  if (tid < a.n) {
+    const int at = group * a.n + tid;
     a.out_scores[at] = out_s;
     a.out_parents[at] = parent;
     a.out_tokens[at] = token;
@@ -439,17 +478,14 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(BeamArgs a) {
 
 template <int DT>
 hipError_t launch(const BeamArgs& a, hipStream_t st) {
-  const int64_t waves = (int64_t)a.groups * a.beams * a.n_parts;
-  beam_parts_kernel<DT><<<dim3((unsigned)((waves + 3) / 4)), 256, 0, st>>>(a);
+  const int rows = a.groups * a.beams;
+  beam_parts_kernel<DT><<<dim3((unsigned)(((int64_t)rows * a.n_parts + 3) / 4)), 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int join = a.beams < 16 ? a.beams : 16;
-  const size_t lds = join * sizeof(JoinWave) + (size_t)a.beams * (sizeof(RowOffer) + a.n * (sizeof(uint2) + sizeof(uint64_t)));
-  if (lds > 65536) {
-    e = hipFuncSetAttribute(reinterpret_cast<const void*>(&beam_join_kernel<DT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
-  beam_join_kernel<DT><<<dim3((unsigned)a.groups), join * kWave, lds, st>>>(a);
+  beam_join_kernel<DT><<<dim3((unsigned)rows), kJoinThreads, 0, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  beam_choose_kernel<<<dim3((unsigned)a.groups), kJoinThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -460,6 +496,16 @@ hipError_t launch(const BeamArgs& a, hipStream_t st) {
 int beam_part_len(int64_t rows, int vocab) {
   const int64_t per = (rows * (((int64_t)vocab + kChunk - 1) / kChunk) + 8191) / 8192;
   return (int)std::min<int64_t>(std::max<int64_t>(per, 1), 1024) * kChunk;
+}
+BeamRange beam_range(double scale) {
+  BeamRange r;
+  r.c = scale * kLog2e;
+  const bool fits = r.c > 0x1p-60 && r.c < 0x1p60;   // (else the borders leave fp32's range)
+  r.low = fits ? (float)(-800.0 / r.c) : INFINITY;
+  r.high = fits ? (float)(900.0 / r.c) : -INFINITY;
+  r.absent = fits ? (float)(-900.0 / r.c) : -INFINITY;
+  r.reach = (float)std::min(500.0 / r.c, 1e38);
+  return r;
 }
 int beam_blocks(int vocab) { return (int)(((int64_t)vocab + kBlock - 1) / kBlock); }
 

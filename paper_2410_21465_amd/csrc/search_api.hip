@@ -42,16 +42,17 @@ bool meet(const Span& a, const Span& b) { return a.p && b.p && a.n && b.n && a.p
 
 struct BeamLayout {
   int part_len, n_parts, n_blocks;
-  size_t peaks, total;
+  size_t peaks, offers, total;
 };
-BeamLayout beam_layout(const shadowkv_logits* x) {
+BeamLayout beam_layout(const shadowkv_logits* x, int n_out) {
   BeamLayout L;
   const int64_t rows = (int64_t)x->n_groups * x->n_beams;
   L.part_len = beam_part_len(rows, x->vocab);
   L.n_parts = (int)(((int64_t)x->vocab + L.part_len - 1) / L.part_len);
   L.n_blocks = beam_blocks(x->vocab);
   L.peaks = up((size_t)rows * L.n_parts * sizeof(BeamPart));
-  L.total = std::max(L.peaks + up((size_t)rows * L.n_blocks * sizeof(uint32_t)), kAlign);
+  L.offers = L.peaks + up((size_t)rows * L.n_blocks * sizeof(uint32_t));
+  L.total = std::max(L.offers + up((size_t)rows * n_out * sizeof(BeamOffer)), kAlign);
   return L;
 }
 
@@ -80,7 +81,7 @@ struct Pieces {
 extern "C" {
 
 size_t shadowkv_beam_select_workspace_bytes(const shadowkv_logits* logits, int32_t n_out) {
-  return check_logits(logits, n_out, false) == SHADOWKV_OK ? beam_layout(logits).total : 0;
+  return check_logits(logits, n_out, false) == SHADOWKV_OK ? beam_layout(logits, n_out).total : 0;
 }
 
 int shadowkv_beam_select(const shadowkv_logits* logits, const float* scores, const uint8_t* finished, const int32_t* lengths, double length_penalty,
@@ -110,7 +111,7 @@ int shadowkv_beam_select(const shadowkv_logits* logits, const float* scores, con
     for (int j = 0; j < i; ++j)
       if (meet(outs[i], outs[j])) return fail_inval("outputs share memory with each other or the workspace");
   }
-  const BeamLayout L = beam_layout(logits);
+  const BeamLayout L = beam_layout(logits, n_out);
   rc = check_workspace(workspace, workspace_bytes, L.total);
   if (rc != SHADOWKV_OK) return rc;
   BeamArgs a{};
@@ -120,12 +121,14 @@ int shadowkv_beam_select(const shadowkv_logits* logits, const float* scores, con
   a.groups = logits->n_groups; a.beams = logits->n_beams; a.vocab = logits->vocab; a.dtype = logits->dtype; a.n = n_out;
   a.part_len = L.part_len; a.n_parts = L.n_parts;
   a.scale = scale; a.penalty = length_penalty;
+  a.range = beam_range(scale);
   a.scores = scores; a.finished = finished; a.lengths = lengths;
   a.end_token = end_token;
   a.out_scores = out_scores; a.out_parents = out_parents; a.out_tokens = out_tokens; a.out_finished = out_finished; a.out_lengths = out_lengths;
   a.parts = static_cast<BeamPart*>(workspace);
   a.n_blocks = L.n_blocks;
   a.peaks = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + L.peaks);
+  a.offers = reinterpret_cast<BeamOffer*>(static_cast<char*>(workspace) + L.offers);
   const hipError_t e = launch_beam_select(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SHADOWKV_OK : fail_hip("beam select", e);
 }
