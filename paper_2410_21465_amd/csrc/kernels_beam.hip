@@ -136,11 +136,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(5, 5))) voi
     if (a.vocab >= kElems) {
       __builtin_memcpy(raw, p + (int64_t)at * EB, kElems * EB);
     } else {
-      uint16_t* half = reinterpret_cast<uint16_t*>(raw);
       for (int e = 0; e < kElems; ++e) {        // token e - (kElems - vocab), as if there were more before it
-        const int64_t t = max(e - (kElems - a.vocab), 0);
-        if constexpr (EB == 4) raw[e] = *reinterpret_cast<const uint32_t*>(p + t * EB);
-        else half[e] = *reinterpret_cast<const uint16_t*>(p + t * EB);
+        const uint8_t* q = p + (int64_t)max(e - (kElems - a.vocab), 0) * EB;   // (volatile: not to be merged with the reads above)
+        if constexpr (EB == 4) {
+          raw[e] = *reinterpret_cast<const volatile uint32_t*>(q);
+        } else {
+          const uint32_t h = *reinterpret_cast<const volatile uint16_t*>(q);
+          raw[e / 2] = e & 1 ? (raw[e / 2] & 0xffffu) | (h << 16) : h;
+        }
       }
     }
   };
@@ -196,11 +199,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(5, 5))) voi
     if (lane % 16 == 15 && (kWhole || block * kBlock < t1 - t0)) peak[block] = m;
     return u;
   };
-  load(t0);                                     // (on its way while it turns out whether the row takes part; the second launch asks the same)
-  if (!row_lives(a.scores[row]) || (a.finished && a.finished[row])) return;
+  load(t0);
+  // (asked after the first chunk, so that its logits do not wait for the answer; the second launch asks the same)
+  const float score = a.scores[row];
+  const uint8_t done = a.finished ? a.finished[row] : 0;
   Sums u{0.0, 0.0, -INFINITY, false};
   int base = t0;
-  for (; base + kChunk <= t1; base += kChunk) u = chunk(std::true_type(), base, u);
+  for (; base + kChunk <= t1; base += kChunk) {
+    u = chunk(std::true_type(), base, u);
+    if (!row_lives(score) || done) return;
+  }
   if (base < t1) u = chunk(std::false_type(), base, u);
   u.far = wave_sum_f64_dpp(u.far);
   u.plain = wave_sum_f64_dpp(u.plain);
