@@ -320,6 +320,7 @@ struct PoolArg {
   int64_t stride;
   int32_t *lens, *refs;
   int batch, per_seq, n_pages, shift;   // shift: log2 of the page size
+  bool refs_aligned;        // to 16 bytes
 };
 struct MovesArg {
   int32_t *src, *dst, *rows;

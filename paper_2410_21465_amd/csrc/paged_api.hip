@@ -253,7 +253,7 @@ int check_moves(const shadowkv_page_moves* m) {
 PoolArg pool_arg(const shadowkv_page_pool* p) {
   int shift = 0;
   while ((1 << shift) < p->page_size) ++shift;
-  return {p->page_table, p->table_stride, p->kv_lens, p->page_refs, p->batch, p->pages_per_seq, p->n_pages, shift};
+  return {p->page_table, p->table_stride, p->kv_lens, p->page_refs, p->batch, p->pages_per_seq, p->n_pages, shift, aligned16(p->page_refs)};
 }
 MovesArg moves_arg(const shadowkv_page_moves* m) { return {m->src, m->dst, m->rows, m->count, m->capacity}; }
 
