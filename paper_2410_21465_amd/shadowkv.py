@@ -623,6 +623,27 @@ class _Launch:
             self._ctx.__exit__(*exc)
 
 
+class _OnCurrent:
+    """What ``_Launch`` is where there is nothing to enter: entering costs a call less."""
+
+    def __init__(self, raw: int):
+        self._raw = raw
+
+    def __enter__(self) -> int:
+        return self._raw
+
+    def __exit__(self, *exc):
+        pass
+
+
+def _launch(device: torch.device, stream):
+    """``_Launch``, or without its costs where the current device and its current stream are meant."""
+    index = device.index
+    if stream is None and index is not None and index == torch._C._cuda_getDevice():
+        return _OnCurrent(torch._C._cuda_getCurrentRawStream(index))
+    return _Launch(device, stream)
+
+
 def rotate(rope: Rope, x: torch.Tensor, out: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
            pos_offset: Optional[torch.Tensor] = None, transposed: bool = False, stream=None) -> torch.Tensor:
     """Heads ``x [seqs, tokens, heads, d]`` (or ``[tokens, heads, d]``) turned to their positions: ``positions [seqs, tokens]``
@@ -666,6 +687,7 @@ class PagedCache:
         self.batch = page_table.shape[0]
         self.c = CPagedCache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], page_table.data_ptr(),
                              page_table.stride(0), self.batch, page_table.shape[1], n, h, d, ps, _DTYPES[k.dtype], 0)
+        self.address, self.n_pages, self.page_size = C.addressof(self.c), n, ps
 
 
 def dense_pages(k: torch.Tensor, v: torch.Tensor, page_size: int) -> PagedCache:
@@ -765,58 +787,58 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n_out: int = 0, fini
     dict, whose scores, finished and lengths may be the arguments themselves where ``n_out`` is ``beams``."""
     if logits.dim() != 3 or logits.dtype not in _LOGITS or not logits.is_cuda:
         raise ValueError("logits must be a bfloat16, float16 or float32 tensor [groups, beams, vocab] on the GPU")
-    groups, beams, vocab = logits.shape
-    sg, sb, sv = logits.stride()
+    (groups, beams, vocab), (sg, sb, sv) = logits.shape, logits.stride()
     if vocab > 1 and sv != 1:
         raise ValueError("the logits of a beam must be contiguous")
-    dev = logits.device
-    _want(scores, "scores", torch.float32, (groups, beams), dev)
+    dev, n, rows = logits.device, n_out or beams, (groups, beams)
+    _want(scores, "scores", torch.float32, rows, dev)
+    kinds = [("scores", torch.float32), ("parents", torch.int32), ("tokens", torch.int32)]
     if finished is not None:
-        _want(finished, "finished", torch.bool, (groups, beams), dev)
+        _want(finished, "finished", torch.bool, rows, dev)
+    if finished is not None or end_token >= 0:
+        kinds.append(("finished", torch.bool))
     if lengths is not None:
-        _want(lengths, "lengths", torch.int32, (groups, beams), dev)
-    n = n_out or beams
-    c = CLogits(logits.data_ptr(), sg, sb, groups, beams, vocab, _LOGITS[logits.dtype])
-    need = int(lib().shadowkv_beam_select_workspace_bytes(C.byref(c), n))
+        _want(lengths, "lengths", torch.int32, rows, dev)
+        kinds.append(("lengths", torch.int32))
+    c = C.byref(CLogits(logits.data_ptr(), sg, sb, groups, beams, vocab, _LOGITS[logits.dtype]))
+    L = lib()
+    need = L.shadowkv_beam_select_workspace_bytes(c, n)
     if need == 0:
         raise ShadowKVError(EINVAL, last_error())
-    kinds = {"scores": torch.float32, "parents": torch.int32, "tokens": torch.int32}
-    if finished is not None or end_token >= 0:
-        kinds["finished"] = torch.bool
-    if lengths is not None:
-        kinds["lengths"] = torch.int32
-    with _Launch(dev, stream) as st:
+    with _launch(dev, stream) as st:
         if out is None:
-            out = {name: torch.empty(groups, n, dtype=kind, device=dev) for name, kind in kinds.items()}
+            out = {name: torch.empty((groups, n), dtype=kind, device=dev) for name, kind in kinds}
         else:
-            if out.keys() != kinds.keys():
-                raise ValueError(f"out must have {', '.join(kinds)}")
-            for name, kind in kinds.items():
+            if out.keys() != dict(kinds).keys():
+                raise ValueError(f"out must have {', '.join(k for k, _ in kinds)}")
+            for name, kind in kinds:
                 _want(out[name], name, kind, (groups, n), dev)
         if workspace is None:
-            workspace = alloc_workspace(need, dev)
+            workspace, room = torch.empty(need, dtype=torch.uint8, device=dev), need
         elif workspace.device != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous tensor on {dev}")
-        _check(lib().shadowkv_beam_select(
-            C.byref(c), scores.data_ptr(), None if finished is None else finished.data_ptr(), None if lengths is None else lengths.data_ptr(),
-            float(length_penalty), float(logit_scale), int(end_token), n, out["scores"].data_ptr(), out["parents"].data_ptr(),
-            out["tokens"].data_ptr(), out["finished"].data_ptr() if "finished" in out else None,
-            out["lengths"].data_ptr() if "lengths" in out else None, workspace.data_ptr(), workspace.numel() * workspace.element_size(), st))
+        else:
+            room = workspace.numel() * workspace.element_size()
+        f, l = out.get("finished"), out.get("lengths")
+        _check(L.shadowkv_beam_select(
+            c, scores.data_ptr(), None if finished is None else finished.data_ptr(), None if lengths is None else lengths.data_ptr(),
+            length_penalty, logit_scale, end_token, n, out["scores"].data_ptr(), out["parents"].data_ptr(), out["tokens"].data_ptr(),
+            None if f is None else f.data_ptr(), None if l is None else l.data_ptr(), workspace.data_ptr(), room, st))
     return out
 
 
-def _rows(t: torch.Tensor, n: int, device) -> CRows:
-    """[rows, ...] as ``shadowkv_rows``: what follows the rows has to be pieces of contiguous elements at one stride."""
-    if t.dim() == 0 or t.shape[0] != n:
-        raise ValueError(f"an array must have {n} rows, not shape {tuple(t.shape)}")
-    if not t.is_cuda or t.device != device:
+def _rows(t: torch.Tensor, n: int, device) -> tuple:
+    """[rows, ...] as the fields of ``shadowkv_rows``: what follows the rows has to be pieces of contiguous elements at one stride."""
+    shape = t.shape
+    if not shape or shape[0] != n:
+        raise ValueError(f"an array must have {n} rows, not shape {tuple(shape)}")
+    if t.device != device:
         raise ValueError(f"an array must be on {device}, not {t.device}")
-    eb, inner, outer, step = t.element_size(), 1, 1, 0
-    if t.numel() == 0:
-        return CRows(None, 0, 0, 0, 0, 0)
-    if t[0].is_contiguous():
-        return CRows(t.data_ptr(), t.stride(0) * eb, 0, t.numel() // n * eb, 1, 0)
-    dims = [(s, d) for s, d in zip(t.shape[1:], t.stride()[1:]) if s != 1]
+    if t.is_contiguous():
+        each = t.nbytes // n if n else 0
+        return t.data_ptr(), each, 0, each, 1
+    stride, eb, inner, outer, step = t.stride(), t.element_size(), 1, 1, 0
+    dims = [(s, d) for s, d in zip(shape[1:], stride[1:]) if s != 1]
     while dims and dims[-1][1] == inner:
         inner *= dims.pop()[0]
     if dims:
@@ -824,26 +846,29 @@ def _rows(t: torch.Tensor, n: int, device) -> CRows:
     while dims and dims[-1][1] == outer * step:
         outer *= dims.pop()[0]
     if dims:
-        raise ValueError(f"rows of shape {tuple(t.shape[1:])} and strides {t.stride()[1:]} are not pieces at one stride")
-    return CRows(t.data_ptr(), t.stride(0) * eb, step * eb, inner * eb, outer, 0)
+        raise ValueError(f"rows of shape {tuple(shape[1:])} and strides {stride[1:]} are not pieces at one stride")
+    return t.data_ptr(), stride[0] * eb, step * eb, inner * eb, outer
 
 
 def reorder_rows(arrays, parents: torch.Tensor, stream=None) -> None:
     """Row i of every tensor of ``arrays`` (one tensor or several, ``[rows, ...]`` of any types; views such as ``A[:, prompt:]`` or
     ``k[:, :, -32:]`` too) becomes what row ``parents[i]`` was, in place.  ``parents`` int32, as many as rows (``[groups, beams]`` of
     ``beam_select``, say); rows with a parent outside stay as they are."""
-    arrays = [arrays] if isinstance(arrays, torch.Tensor) else list(arrays)
+    arrays = [arrays] if isinstance(arrays, torch.Tensor) else arrays
     n, dev = parents.numel(), parents.device
     _want(parents, "parents", torch.int32, parents.shape)
-    rows = (CRows * max(len(arrays), 1))(*(_rows(t, n, dev) for t in arrays))
-    with _Launch(dev, stream) as st:
-        _check(lib().shadowkv_reorder_rows(rows, len(arrays), parents.data_ptr(), n, st))
+    fields = []
+    for t in arrays:
+        fields += _rows(t, n, dev)
+    rows = (C.c_int64 * max(len(fields), 1))(*fields)        # five to an array; the upper half of the last is `reserved`
+    with _launch(dev, stream) as st:
+        _check(lib().shadowkv_reorder_rows(rows, len(fields) // 5, parents.data_ptr(), n, st))
 
 
-def _pages_copy(caches, to, moves: CPageMoves, st) -> None:
-    ptrs = C.POINTER(CPagedCache) * max(len(caches), 1)
-    frm = ptrs(*(C.pointer(c.c) for c in caches))
-    _check(lib().shadowkv_pages_copy(frm, frm if to is caches else ptrs(*(C.pointer(c.c) for c in to)), len(caches), C.byref(moves), st))
+def _pages_copy(caches, to, moves, st) -> None:
+    ptrs = C.c_void_p * max(len(caches), 1)
+    frm = ptrs(*[c.address for c in caches])
+    _check(lib().shadowkv_pages_copy(frm, frm if to is caches else ptrs(*[c.address for c in to]), len(caches), moves, st))
 
 
 def pages_copy(caches, src: torch.Tensor, dst: torch.Tensor, rows: Optional[torch.Tensor] = None, to=None, stream=None) -> None:
@@ -861,8 +886,8 @@ def pages_copy(caches, src: torch.Tensor, dst: torch.Tensor, rows: Optional[torc
         _want(rows, "rows", torch.int32, src.shape, dev)
     if any(c.device != dev for c in caches) or any(c.device != dev for c in to):
         raise ValueError(f"the caches must be on {dev}")
-    with _Launch(dev, stream) as st:
-        _pages_copy(caches, to, CPageMoves(src.data_ptr(), dst.data_ptr(), None if rows is None else rows.data_ptr(), None, src.numel(), 0), st)
+    with _launch(dev, stream) as st:
+        _pages_copy(caches, to, C.byref(CPageMoves(src.data_ptr(), dst.data_ptr(), None if rows is None else rows.data_ptr(), None, src.numel(), 0)), st)
 
 
 class PagePool:
@@ -887,7 +912,9 @@ class PagePool:
         self.move_src, self.move_dst, self.move_rows, self.move_count, self.n_used = ints(room), ints(room), ints(room), ints(1), ints(1)
         self.workspace = alloc_workspace(need, self.device)
         c.page_table, c.kv_lens, c.page_refs = self.page_table.data_ptr(), self.kv_lens.data_ptr(), self.page_refs.data_ptr()
-        self.c = c
+        moves = [CPageMoves(self.move_src.data_ptr(), self.move_dst.data_ptr(), self.move_rows.data_ptr(), self.move_count.data_ptr(), most, 0)
+                 for most in (batch, room)]
+        self._c, self._update_moves, self._compact_moves = C.byref(c), C.byref(moves[0]), C.byref(moves[1])
 
     def cache(self, k: torch.Tensor, v: torch.Tensor) -> PagedCache:
         """``PagedCache`` of a layer's pages ``k, v [n_pages, h_kv, page_size, d]`` under this pool's table."""
@@ -898,40 +925,36 @@ class PagePool:
     def _layers(self, caches) -> list:
         caches = [caches] if isinstance(caches, PagedCache) else list(caches)
         for c in caches:
-            if c.device != self.device or c.c.page_size != self.page_size or c.c.n_pages < self.n_pages:
+            if c.page_size != self.page_size or c.n_pages < self.n_pages or c.device != self.device:
                 raise ValueError(f"a cache must have {self.n_pages} pages of {self.page_size} tokens on {self.device}")
         return caches
-
-    def _moves(self, room: int) -> CPageMoves:
-        return CPageMoves(self.move_src.data_ptr(), self.move_dst.data_ptr(), self.move_rows.data_ptr(), self.move_count.data_ptr(), room, 0)
 
     def update(self, parents: Optional[torch.Tensor] = None, keep_lens: Optional[torch.Tensor] = None, n_new=0, caches=(), stream=None) -> None:
         """Row i becomes the first ``min(kv_lens[parents[i]], keep_lens[i])`` tokens of what row ``parents[i]`` was (empty where that is
         outside the batch), with room for ``n_new`` (a number, or int32 ``[batch]``) further ones, which ``kv_lens`` then counts, as
         ``paged_append`` wants it; a row that the pages do not suffice for gets none.  Copies, in every cache of ``caches``, the last pages that
         rows share and are about to write."""
-        for name, t in (("parents", parents), ("keep_lens", keep_lens), ("n_new", n_new)):
-            if isinstance(t, torch.Tensor) and t.numel() != self.batch:
-                raise ValueError(f"{name} must have {self.batch} elements, not {t.numel()}")
-            if isinstance(t, torch.Tensor):
-                _want(t, name, torch.int32, t.shape, self.device)
         each = isinstance(n_new, torch.Tensor)
-        caches, moves = self._layers(caches), self._moves(self.batch)
-        with _Launch(self.device, stream) as st:
-            _check(lib().shadowkv_pages_update(C.byref(self.c), None if parents is None else parents.data_ptr(),
+        for name, t in (("parents", parents), ("keep_lens", keep_lens), ("n_new", n_new if each else None)):
+            if t is not None:
+                if t.numel() != self.batch:
+                    raise ValueError(f"{name} must have {self.batch} elements, not {t.numel()}")
+                _want(t, name, torch.int32, t.shape, self.device)
+        caches = self._layers(caches)
+        with _launch(self.device, stream) as st:
+            _check(lib().shadowkv_pages_update(self._c, None if parents is None else parents.data_ptr(),
                                                None if keep_lens is None else keep_lens.data_ptr(), n_new.data_ptr() if each else None,
-                                               0 if each else int(n_new), C.byref(moves), self.workspace.data_ptr(), self.workspace.numel(), st))
+                                               0 if each else int(n_new), self._update_moves, self.workspace.data_ptr(), self.workspace.numel(), st))
             if caches:
-                _pages_copy(caches, caches, moves, st)
+                _pages_copy(caches, caches, self._update_moves, st)
 
     def compact(self, max_moves: Optional[int] = None, caches=(), stream=None) -> torch.Tensor:
         """Moves the highest used pages into the lowest free ones (at most ``max_moves``), in every cache of ``caches``.  Returns ``n_used [1]``
         int32 on the device: all pages from there on are free."""
-        room = self.move_src.numel()
-        caches, moves = self._layers(caches), self._moves(room)
-        with _Launch(self.device, stream) as st:
-            _check(lib().shadowkv_pages_compact(C.byref(self.c), room if max_moves is None else int(max_moves), C.byref(moves), self.n_used.data_ptr(),
+        room, caches = self.move_src.numel(), self._layers(caches)
+        with _launch(self.device, stream) as st:
+            _check(lib().shadowkv_pages_compact(self._c, room if max_moves is None else int(max_moves), self._compact_moves, self.n_used.data_ptr(),
                                                 self.workspace.data_ptr(), self.workspace.numel(), st))
             if caches:
-                _pages_copy(caches, caches, moves, st)
+                _pages_copy(caches, caches, self._compact_moves, st)
         return self.n_used
