@@ -3,7 +3,7 @@
 // Three launches.  The first reads the logits once: a wave takes a part of a row, sums its exponentials (fp64) and keeps the largest logit of
 // every block of 256 tokens, nothing else.  The second has a workgroup per row.  The n best tokens of a row lie in the n blocks with the
 // largest maxima (whatever lies in another block has n better ones, one in each of those), so it finds these, reads them again, and
-// keeps their n best.  The third, a workgroup per group, ranks what all rows offer.  (Done by the group's last workgroup of the second launch instead,
+// keeps their n best.  The third, a workgroup per group, ranks what all rows offer; small calls do both in one launch.  (Done by the group's last workgroup of the second launch instead,
 // behind a counter, the choice costs more than its launch: every workgroup has to write its L2 back first.  32 x 16 rows: 82 us for
 // both.)
 //
@@ -216,36 +216,53 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(5, 5))) voi
   if (lane == 0) a.parts[w] = BeamPart{u.plain, u.far, u.ref, bad};
 }
 
-// ---- the n largest of many keys, by a workgroup --------------------------------------------------------------------------
+// ---- the n largest of many keys, by a team: a workgroup (T = 256) or a wave (T = 64) ----------------------------------------------
 // What reaches a bound that n keys reach, and few others do, is put into LDS and sorted by counting, for each, what is larger.  Keys are 64 bits
 // wide, 0 is none; they come with a number, and of equal keys the lower number goes first (kTies; other keys are never equal).
-constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / kWave;
+constexpr int kJoinThreads = 256;
+struct RowSum {
+  double log_sum;
+  float ref;
+};
+template <int T>
 struct __align__(16) JoinRoom {
-  uint64_t key[kJoinThreads];
-  uint32_t item[kJoinThreads];
-  uint32_t upper[kJoinThreads];
+  static constexpr int kRoom = T == kWave ? 128 : 256;
+  uint64_t key[kRoom];
+  uint32_t item[kRoom];
+  uint32_t upper[T];
   uint64_t best[64];                                      // what comes out, in order
   uint32_t best_item[64];
+  RowSum sum;
   uint32_t bound;
   int count, other;
 };
-__device__ __forceinline__ void take(uint64_t k, uint32_t item, bool takes, JoinRoom& room, int lane) {
+template <int T>
+__device__ __forceinline__ void team_sync() {
+  if constexpr (T == kWave) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  } else {
+    __syncthreads();
+  }
+}
+template <int T>
+__device__ __forceinline__ void take(uint64_t k, uint32_t item, bool takes, JoinRoom<T>& room, int lane) {
   const uint64_t taken = __ballot(takes);
   if (taken == 0) return;
   int at = 0;
   if (lane == 0) at = atomicAdd(&room.count, __popcll(taken));
   at = __builtin_amdgcn_readfirstlane(at) + __popcll(taken & ((1ull << lane) - 1));
-  if (takes && at < kJoinThreads) { room.key[at] = k; room.item[at] = item; }
+  if (takes && at < JoinRoom<T>::kRoom) { room.key[at] = k; room.item[at] = item; }
 }
 // what is in the room, in order; all threads, after a barrier
-template <bool kTies>
-__device__ __forceinline__ int sort_room(JoinRoom& room, int n, int tid) {
+template <bool kTies, int T>
+__device__ __forceinline__ int sort_room(JoinRoom<T>& room, int n, int tid) {
   const int c = room.count;
-  if (tid >= c && tid < ((c + 7) & ~7)) { room.key[tid] = 0; room.item[tid] = ~0u; }
-  __syncthreads();
-  if (tid < c) {
-    const uint64_t k = room.key[tid];
-    const uint32_t item = room.item[tid];
+  if (c + tid < ((c + 7) & ~7)) { room.key[c + tid] = 0; room.item[c + tid] = ~0u; }
+  team_sync<T>();
+  for (int i = tid; i < c; i += T) {
+    const uint64_t k = room.key[i];
+    const uint32_t item = room.item[i];
     int rank = 0;
     for (int j = 0; j < c; j += 8) {
 #pragma unroll
@@ -261,29 +278,32 @@ __device__ __forceinline__ int sort_room(JoinRoom& room, int n, int tid) {
     }
     if (rank < n) { room.best[rank] = k; room.best_item[rank] = item; }
   }
-  __syncthreads();
+  team_sync<T>();
   return min(c, n);
 }
 // A key that n keys reach, from the upper halves (at least 1: a key of 0 is none): the n-th largest of the threads' own largest, or up to kFewPlaces
 // places, which 64 values are enough for, of the largest of four threads.
 constexpr int kFewPlaces = 16;
-__device__ __forceinline__ uint64_t find_bound(uint64_t largest, int n, JoinRoom& room, int tid) {
+template <int T>
+__device__ __forceinline__ uint64_t find_bound(uint64_t largest, int n, JoinRoom<T>& room, int tid) {
   const int lane = tid & (kWave - 1);
   uint32_t mine = (uint32_t)(largest >> 32), bound;
-  room.upper[tid] = mine;
-  if (tid == 0) { room.count = 0; room.bound = ~0u; }
-  __syncthreads();
   int larger = 0;
-  if (n <= kFewPlaces) {                                  // (every wave finds it by itself)
-    mine = room.upper[lane];
+  if (tid == 0) { room.count = 0; room.bound = ~0u; }
+  if constexpr (T > kWave) room.upper[tid] = mine;
+  team_sync<T>();
+  if (T == kWave || n <= kFewPlaces) {                    // (every wave finds it by itself)
+    if constexpr (T > kWave) {
+      mine = room.upper[lane];
 #pragma unroll
-    for (int v = 1; v < kJoinWaves; ++v) mine = op_max(mine, room.upper[v * kWave + lane]);
+      for (int v = 1; v < T / kWave; ++v) mine = op_max(mine, room.upper[v * kWave + lane]);
+    }
 #pragma unroll 8
     for (int j = 0; j < kWave; ++j) larger += (uint32_t)__builtin_amdgcn_readlane((int)mine, j) > mine;
     bound = wave_min_u32(larger < n ? mine : ~0u);
   } else {
 #pragma unroll 4
-    for (int j = 0; j < kJoinThreads; j += 4) {
+    for (int j = 0; j < T; j += 4) {
       const uint4 o = *reinterpret_cast<const uint4*>(&room.upper[j]);
       larger += o.x > mine;
       larger += o.y > mine;
@@ -292,29 +312,29 @@ __device__ __forceinline__ uint64_t find_bound(uint64_t largest, int n, JoinRoom
     }
     const uint32_t least = wave_min_u32(larger < n ? mine : ~0u);
     if (lane == 0) atomicMin(&room.bound, least);
-    __syncthreads();
+    team_sync<T>();
     bound = room.bound;
   }
   return bound ? (uint64_t)bound << 32 : 1;
 }
 // Where more reach the bound than there is room for (many equal ones, say): the largest bound that n keys reach, bit by bit, and of the keys that
 // equal it the lowest numbers.  key(i, item): of entry i < n_entries, and its number.
-template <bool kTies, class Key>
-__device__ __forceinline__ void take_exactly(Key key, int n_entries, int n, uint64_t bound, JoinRoom& room, int tid) {
+template <bool kTies, int T, class Key>
+__device__ __forceinline__ void take_exactly(Key key, int n_entries, int n, uint64_t bound, JoinRoom<T>& room, int tid) {
   const int lane = tid & (kWave - 1);
   // how many are above `from`, or equal it and have a number below `below`
   auto count = [&](uint64_t from, uint32_t below) {
-    __syncthreads();
+    team_sync<T>();
     if (tid == 0) room.other = 0;
-    __syncthreads();
+    team_sync<T>();
     int c = 0;
-    for (int i = tid; i < n_entries; i += kJoinThreads) {
+    for (int i = tid; i < n_entries; i += T) {
       uint32_t item = 0;
       const uint64_t k = key(i, item);
       c += k > from || (k == from && item < below);
     }
     if (c) atomicAdd(&room.other, c);
-    __syncthreads();
+    team_sync<T>();
     return room.other;
   };
   for (int b = 63; b >= 0; --b) {
@@ -329,78 +349,73 @@ __device__ __forceinline__ void take_exactly(Key key, int n_entries, int n, uint
     ++below;
   }
   if (tid == 0) room.count = 0;
-  __syncthreads();
-  for (int i0 = 0; i0 < n_entries; i0 += kJoinThreads) {
+  team_sync<T>();
+  for (int i0 = 0; i0 < n_entries; i0 += T) {
     uint32_t item = 0;
     const uint64_t k = i0 + tid < n_entries ? key(i0 + tid, item) : 0;
     take(k, item, k > bound || (k == bound && item < below), room, lane);
   }
-  __syncthreads();
+  team_sync<T>();
 }
-template <bool kTies, class Key>
-__device__ __forceinline__ int top_items(Key key, int n_entries, int n, JoinRoom& room, int tid) {
+template <bool kTies, int T, class Key>
+__device__ __forceinline__ int top_items(Key key, int n_entries, int n, JoinRoom<T>& room, int tid) {
   const int lane = tid & (kWave - 1);
   uint64_t mine = 0;
   uint32_t item = 0;
 #pragma unroll 4
-  for (int i = tid; i < n_entries; i += kJoinThreads) { const uint64_t k = key(i, item); mine = k > mine ? k : mine; }
+  for (int i = tid; i < n_entries; i += T) { const uint64_t k = key(i, item); mine = k > mine ? k : mine; }
   const uint64_t bound = find_bound(mine, n, room, tid);
 #pragma unroll 4
-  for (int i0 = 0; i0 < n_entries; i0 += kJoinThreads) {
+  for (int i0 = 0; i0 < n_entries; i0 += T) {
     const uint64_t k = i0 + tid < n_entries ? key(i0 + tid, item) : 0;
     take(k, item, k >= bound, room, lane);
   }
-  __syncthreads();
-  if (__builtin_expect(room.count > kJoinThreads, 0)) take_exactly<kTies>(key, n_entries, n, bound, room, tid);
+  team_sync<T>();
+  if (__builtin_expect(room.count > JoinRoom<T>::kRoom, 0)) take_exactly<kTies>(key, n_entries, n, bound, room, tid);
   return sort_room<kTies>(room, n, tid);
 }
 
-template <int DT>
-__global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
-  constexpr int EB = Logit<DT>::bytes, kEach = 8, kLanes = kBlock / kEach, kAtOnce = kJoinThreads / kLanes;
-  __shared__ JoinRoom room;
-  __shared__ double base_shared;
-  __shared__ float ref_shared;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, row = blockIdx.x, group = row / a.beams;
-  const double c_log2 = a.range.c;
+// log of a row's sum of exponentials relative to `ref`, by a wave; ref = -inf: the row offers nothing
+__device__ __forceinline__ RowSum row_sum(const BeamArgs& a, int row, int lane) {
+  const BeamPart* parts = a.parts + (int64_t)row * a.n_parts;
+  const double c = a.range.c;
+  bool bad = false, plain = false;
+  float ref = -INFINITY;
+  for (int i = lane; i < a.n_parts; i += kWave) {
+    const BeamPart q = parts[i];
+    bad |= q.bad != 0;
+    plain |= q.plain > 0.0;
+    ref = fmaxf(ref, q.ref);
+  }
+  ref = wave_max_f32(ref);
+  if (__ballot(plain)) ref = fmaxf(ref, 0.f);             // (plain sums are relative to a logit of 0)
+  if (__ballot(bad) || ref == -INFINITY) return RowSum{0.0, -INFINITY};
+  double sum = 0.0;
+  for (int i = lane; i < a.n_parts; i += kWave) {
+    const BeamPart q = parts[i];
+    sum += q.plain * exp2_f64(-(double)ref * c);
+    if (q.ref > -INFINITY) sum += q.sum * exp2_f64(((double)q.ref - (double)ref) * c);
+  }
+  return RowSum{log(wave_sum_f64_dpp(sum)), ref};
+}
+
+// what a row offers, in order, n places, by a team
+template <int DT, int T>
+__device__ __forceinline__ void row_offers(const BeamArgs& a, int row, JoinRoom<T>& room, BeamOffer* offer, int tid) {
+  constexpr int EB = Logit<DT>::bytes, kEach = 8, kLanes = kBlock / kEach, kAtOnce = T / kLanes;
+  const int lane = tid & (kWave - 1), wave = tid >> 6, group = row / a.beams;
   const float s = a.scores[row];
   const bool lives = row_lives(s), done = a.finished && a.finished[row];
   double weight = 1.0;
   if (a.penalty != 0.0) weight = pow(fmax((double)a.lengths[row] + (done ? 0.0 : 1.0), 1.0), a.penalty);
-  BeamOffer* offer = a.offers + (int64_t)row * a.n;
   int count = 0;
   if (lives && done) {
     count = 1;
     if (tid == 0) offer[0] = BeamOffer{f64_key((double)s / weight), s, a.end_token};
   } else if (lives) {
-    // the row's sum, by one wave, while the others go ahead
-    if (wave == kJoinWaves - 1) {
-      const BeamPart* parts = a.parts + (int64_t)row * a.n_parts;
-      bool bad = false, plain = false;
-      float ref = -INFINITY;
-      for (int i = lane; i < a.n_parts; i += kWave) {
-        const BeamPart q = parts[i];
-        bad |= q.bad != 0;
-        plain |= q.plain > 0.0;
-        ref = fmaxf(ref, q.ref);
-      }
-      ref = wave_max_f32(ref);
-      if (__ballot(plain)) ref = fmaxf(ref, 0.f);         // (plain sums are relative to a logit of 0)
-      double sum = 0.0;
-      if (!__ballot(bad) && ref > -INFINITY) {
-        for (int i = lane; i < a.n_parts; i += kWave) {
-          const BeamPart q = parts[i];
-          sum += q.plain * exp2_f64(-(double)ref * c_log2);
-          if (q.ref > -INFINITY) sum += q.sum * exp2_f64(((double)q.ref - (double)ref) * c_log2);
-        }
-        sum = wave_sum_f64_dpp(sum);
-      } else {
-        ref = -INFINITY;                                  // nothing is offered
-      }
-      if (lane == 0) {
-        base_shared = (double)s - log(sum);
-        ref_shared = ref;
-      }
+    if (wave == T / kWave - 1) {                          // (the other waves of a workgroup go ahead)
+      const RowSum sum = row_sum(a, row, lane);
+      if (lane == 0) room.sum = sum;
     }
     const uint8_t* p = a.logits + (int64_t)group * a.group_stride + (int64_t)(row % a.beams) * a.beam_stride;
     // (logit, ~number): among equal logits the lower token or block goes first
@@ -415,7 +430,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
       // tokens of those blocks that are not less than the n-th block's largest
       const uint64_t bound = n_best == a.n ? room.best[n_best - 1] >> 32 << 32 : 1;
       if (tid == 0) room.count = 0;
-      __syncthreads();
+      team_sync<T>();
       for (int i0 = 0; i0 < n_best; i0 += kAtOnce) {
         const int i = i0 + tid / kLanes;
         const int at = i < n_best ? block(i) * kBlock + tid % kLanes * kEach : a.vocab;
@@ -434,27 +449,27 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
           take(k, 0, k >= bound, room, lane);
         }
       }
-      __syncthreads();
-      if (__builtin_expect(room.count > kJoinThreads, 0))
+      team_sync<T>();
+      if (__builtin_expect(room.count > JoinRoom<T>::kRoom, 0))
         take_exactly<false>([&](int i, uint32_t& item) -> uint64_t {
           const int t = block(i / kBlock) * kBlock + i % kBlock;
           return t < a.vocab ? token_key(t, item) : 0;
         }, n_best * kBlock, a.n, bound, room, tid);
       count = sort_room<false>(room, a.n, tid);
     }
-    if (ref_shared == -INFINITY) count = 0;
+    const RowSum sum = room.sum;
+    if (sum.ref == -INFINITY) count = 0;
     if (tid < count) {
-      const double score = base_shared + a.scale * ((double)key_f32((uint32_t)(room.best[tid] >> 32)) - (double)ref_shared);
+      const double score = (double)s - sum.log_sum + a.scale * ((double)key_f32((uint32_t)(room.best[tid] >> 32)) - (double)sum.ref);
       offer[tid] = BeamOffer{f64_key(score / weight), (float)score, (int32_t)~(uint32_t)room.best[tid]};
     }
   }
   if (tid >= count && tid < a.n) offer[tid] = BeamOffer{0, -INFINITY, -1};
 }
 
-__global__ __launch_bounds__(kJoinThreads) void beam_choose_kernel(BeamArgs a) {
-  __shared__ JoinRoom room;
-  const int tid = threadIdx.x, group = blockIdx.x;
-  const BeamOffer* all = a.offers + (int64_t)group * a.beams * a.n;
+// of what the rows of a group offer, the best
+template <int T>
+__device__ __forceinline__ void choose(const BeamArgs& a, int group, const BeamOffer* all, JoinRoom<T>& room, int tid) {
   const int found = top_items<true>([&](int i, uint32_t& item) -> uint64_t {
     item = (uint32_t)i;                                   // in order of rows, then of places
     return all[i].rank;
@@ -485,11 +500,38 @@ __global__ __launch_bounds__(kJoinThreads) void beam_choose_kernel(BeamArgs a) {
 }
 
 template <int DT>
+__global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
+  __shared__ JoinRoom<kJoinThreads> room;
+  row_offers<DT>(a, blockIdx.x, room, a.offers + (int64_t)blockIdx.x * a.n, threadIdx.x);
+}
+__global__ __launch_bounds__(kJoinThreads) void beam_choose_kernel(BeamArgs a) {
+  __shared__ JoinRoom<kJoinThreads> room;
+  choose(a, blockIdx.x, a.offers + (int64_t)blockIdx.x * a.beams * a.n, room, threadIdx.x);
+}
+// both in one launch, a wave for each of a group's rows: where there is little to look through a launch less counts for more than three waves less
+// a row.  A call at 1 x 4 x 32000, 4 / 8 / 16 places: 15.2 / 15.8 / 20.3 us, 17.5 apart; 16 x 4 x 50257, 4 places: 18.2 and 17.6;
+// 64 x 8 x 8000, 8 places: 18.6 and 17.8.
+constexpr int kFewBeams = 4, kFewInOne = 8, kFewBlocks = 128;
+template <int DT>
+__global__ __launch_bounds__(kFewBeams * kWave) void beam_finish_kernel(BeamArgs a) {
+  __shared__ JoinRoom<kWave> rooms[kFewBeams];
+  __shared__ BeamOffer offers[kFewBeams * kFewInOne];
+  const int b = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & (kWave - 1);
+  row_offers<DT>(a, blockIdx.x * a.beams + b, rooms[b], offers + b * a.n, lane);
+  __syncthreads();
+  if (b == 0) choose(a, blockIdx.x, offers, rooms[0], lane);
+}
+
+template <int DT>
 hipError_t launch(const BeamArgs& a, hipStream_t st) {
   const int rows = a.groups * a.beams;
   beam_parts_kernel<DT><<<dim3((unsigned)(((int64_t)rows * a.n_parts + 3) / 4)), 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  if (a.beams <= kFewBeams && a.n <= kFewInOne && a.n_blocks <= kFewBlocks) {
+    beam_finish_kernel<DT><<<dim3((unsigned)a.groups), a.beams * kWave, 0, st>>>(a);
+    return hipGetLastError();
+  }
   beam_join_kernel<DT><<<dim3((unsigned)rows), kJoinThreads, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;

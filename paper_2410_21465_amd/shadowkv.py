@@ -807,7 +807,12 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n_out: int = 0, fini
         raise ShadowKVError(EINVAL, last_error())
     with _launch(dev, stream) as st:
         if out is None:
-            out = {name: torch.empty((groups, n), dtype=kind, device=dev) for name, kind in kinds}
+            whole = torch.empty((3 if lengths is None else 4, groups, n), dtype=torch.int32, device=dev).unbind(0)   # (one allocation)
+            out = {"scores": whole[0].view(torch.float32), "parents": whole[1], "tokens": whole[2]}
+            if lengths is not None:
+                out["lengths"] = whole[3]
+            if len(kinds) > len(out):
+                out["finished"] = torch.empty((groups, n), dtype=torch.bool, device=dev)
         else:
             if out.keys() != dict(kinds).keys():
                 raise ValueError(f"out must have {', '.join(k for k, _ in kinds)}")
