@@ -308,8 +308,8 @@ struct ReorderArray {
   int32_t n_outer, unit;    // unit: 16, 4 or 1 bytes
 };
 struct ReorderArgs {
-  ReorderArray a[kMaxReorderArrays];
-  int n_arrays, n_rows;
+  ReorderArray a[kMaxReorderArrays];   // those of 16-byte units first
+  int n_arrays, n_wide, n_rows;
   const int32_t* parents;
 };
 hipError_t launch_reorder_rows(const ReorderArgs& a, hipStream_t st);

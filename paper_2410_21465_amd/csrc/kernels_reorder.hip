@@ -14,25 +14,44 @@ constexpr int kHeld = 8;                                  // pieces of a thread
 constexpr int kSlots = kThreads * kHeld;                  // >= kMaxReorderRows: a slice is one unit wide at least
 static_assert(kSlots >= kMaxReorderRows, "a slice holds a unit of every row");
 
+// Columns first .. first + 2^shift - 1 (in units) of a piece of all rows that change.
+struct Slice {
+  uint8_t* base;
+  int64_t row, first, units;
+};
 template <class T>
-__device__ __forceinline__ void move_slice(const ReorderArray& a, const uint32_t* pairs, int n, int shift, int64_t first, int outer) {
-  T held[kHeld];
-  const int cols = 1 << shift;
-  uint8_t* base = a.p + outer * a.outer;
+struct Held {
+  T x[kHeld];
+};
+template <class T>
+__device__ __forceinline__ Held<T> load_slice(const Slice& s, const uint32_t* pairs, int n, int shift) {
+  Held<T> h;
 #pragma unroll
   for (int k = 0; k < kHeld; ++k) {
     const int item = k * kThreads + threadIdx.x, i = item >> shift;
-    const int64_t u = first + (item & (cols - 1));
-    if (i < n && u < a.units) held[k] = *reinterpret_cast<const T*>(base + (int64_t)(pairs[i] & 0xffffu) * a.row + u * (int64_t)sizeof(T));
+    const int64_t u = s.first + (item & ((1 << shift) - 1));
+    if (i < n && u < s.units) h.x[k] = *reinterpret_cast<const T*>(s.base + (int64_t)(pairs[i] & 0xffffu) * s.row + u * (int64_t)sizeof(T));
   }
-  __builtin_amdgcn_s_waitcnt(0);                          // what is loaded is there before any wave writes
+  return h;
+}
+template <class T>
+__device__ __forceinline__ void store_slice(const Slice& s, const Held<T>& h, const uint32_t* pairs, int n, int shift) {
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const int item = k * kThreads + threadIdx.x, i = item >> shift;
+    const int64_t u = s.first + (item & ((1 << shift) - 1));
+    if (i < n && u < s.units) *reinterpret_cast<T*>(s.base + (int64_t)(pairs[i] >> 16) * s.row + u * (int64_t)sizeof(T)) = h.x[k];
+  }
+}
+// what is loaded is there before any wave writes
+template <class T>
+__device__ __forceinline__ void loaded(const Held<T>& h) {
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    if constexpr (sizeof(T) == 16) asm volatile("" ::"v"(h.x[k].x), "v"(h.x[k].y), "v"(h.x[k].z), "v"(h.x[k].w));
+    else asm volatile("" ::"v"((uint32_t)h.x[k]));
+  }
   __syncthreads();
-#pragma unroll
-  for (int k = 0; k < kHeld; ++k) {
-    const int item = k * kThreads + threadIdx.x, i = item >> shift;
-    const int64_t u = first + (item & (cols - 1));
-    if (i < n && u < a.units) *reinterpret_cast<T*>(base + (int64_t)(pairs[i] >> 16) * a.row + u * (int64_t)sizeof(T)) = held[k];
-  }
 }
 
 __global__ __launch_bounds__(kThreads) void reorder_rows_kernel(ReorderArgs g) {
@@ -67,17 +86,45 @@ __global__ __launch_bounds__(kThreads) void reorder_rows_kernel(ReorderArgs g) {
     }
   }
   __syncthreads();
-  const int64_t total = until[g.n_arrays - 1];
+  const int64_t total = until[g.n_arrays - 1], wide = g.n_wide ? until[g.n_wide - 1] : 0, step = gridDim.x;
   int k = 0;
-  for (int64_t t = blockIdx.x; t < total; t += gridDim.x) {
+  auto slice = [&](int64_t t) {
     while (t >= until[k]) ++k;
-    const ReorderArray a = g.a[k];
+    const ReorderArray& a = g.a[k];
     const int64_t per = (a.units + (1 << shift) - 1) >> shift, in = t - (k ? until[k - 1] : 0);
-    const int outer = (int)(in / per);
-    const int64_t first = (in % per) << shift;
-    if (a.unit == 16) move_slice<uint4>(a, pairs, n, shift, first, outer);
-    else if (a.unit == 4) move_slice<uint32_t>(a, pairs, n, shift, first, outer);
-    else move_slice<uint8_t>(a, pairs, n, shift, first, outer);
+    const int64_t outer = a.n_outer == 1 ? 0 : in / per;
+    return Slice{a.p + outer * a.outer, a.row, (in - outer * per) << shift, a.units};
+  };
+  int64_t t = blockIdx.x;
+  if (t < wide) {                                         // the next slice is on its way while this one is written
+    Slice s = slice(t);
+    Held<uint4> h = load_slice<uint4>(s, pairs, n, shift);
+    for (;;) {
+      t += step;
+      Slice next = s;
+      Held<uint4> h2 = h;
+      if (t < wide) {
+        next = slice(t);
+        h2 = load_slice<uint4>(next, pairs, n, shift);
+      }
+      loaded(h);
+      store_slice(s, h, pairs, n, shift);
+      if (t >= wide) break;
+      s = next;
+      h = h2;
+    }
+  }
+  for (; t < total; t += step) {
+    const Slice s = slice(t);
+    if (g.a[k].unit == 4) {
+      const Held<uint32_t> h = load_slice<uint32_t>(s, pairs, n, shift);
+      loaded(h);
+      store_slice(s, h, pairs, n, shift);
+    } else {
+      const Held<uint8_t> h = load_slice<uint8_t>(s, pairs, n, shift);
+      loaded(h);
+      store_slice(s, h, pairs, n, shift);
+    }
   }
 }
 

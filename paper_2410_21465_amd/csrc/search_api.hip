@@ -178,6 +178,7 @@ int shadowkv_reorder_rows(const shadowkv_rows* arrays, int32_t n_arrays, const i
       r.units = a.inner / r.unit;
     }
     if (g.n_arrays == 0) break;
+    g.n_wide = (int)(std::stable_partition(g.a, g.a + g.n_arrays, [](const ReorderArray& r) { return r.unit == 16; }) - g.a);
     const hipError_t e = launch_reorder_rows(g, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail_hip("reorder rows", e);
   }
