@@ -161,8 +161,10 @@ __global__ __launch_bounds__(kPlanThreads) void pages_grow_kernel(PoolArg p, con
                                                                   int n_new_all, MovesArg m, int32_t* free_list) {
   constexpr int kRows = kFork ? kForkInPlan : kMaxPoolRows, kRowsPerThread = kRows / kPlanThreads;
   __shared__ int32_t lens[kRows];                         // lengths before, then where a row's pages begin in the list
-  __shared__ __align__(16) int tail[kRows];
   __shared__ int first_col[kRows], list_lds[kListRoom];
+  // last pages that rows share and will write, hashed: the rows that will, and the last of them
+  constexpr int kSlots = 2 * kRows;
+  __shared__ int shared_page[kSlots], writers[kSlots], last_writer[kSlots];
   __shared__ ForkRow forks[kFork ? kForkInPlan : 1];
   __shared__ Scan3 sums[kPlanWaves];
   __shared__ int stop, n_granted, n_copied, n_forks, width;   // stop: first row that is not granted
@@ -170,34 +172,41 @@ __global__ __launch_bounds__(kPlanThreads) void pages_grow_kernel(PoolArg p, con
   const int tid = threadIdx.x, rpt = (p.batch + kPlanThreads - 1) / kPlanThreads;
   const int64_t room = (int64_t)p.per_seq << p.shift;
   const int page_mask = (1 << p.shift) - 1;
-  if (tid == 0) { stop = p.batch; n_granted = n_copied = n_forks = width = 0; }
-  for (int i = tid; i < p.batch; i += kPlanThreads) lens[i] = clamp_len(p, p.lens[i]);
+  if (tid == 0) { stop = p.batch; n_forks = width = 0; }
+  for (int i = tid; i < kSlots; i += kPlanThreads) { shared_page[i] = -1; writers[i] = 0; last_writer[i] = -1; }
+  // (all that does not depend on anything is asked for at once)
+  int from[kRowsPerThread], most[kRowsPerThread], grow[kRowsPerThread], kept[kRowsPerThread], page[kRowsPerThread];
+#pragma unroll
+  for (int k = 0; k < kRowsPerThread; ++k) {
+    const int i = tid * rpt + k;
+    from[k] = -1;
+    most[k] = grow[k] = kept[k] = 0;
+    page[k] = -1;
+    if (k < rpt && i < p.batch) {
+      from[k] = parent_of(p, parents, i);
+      most[k] = keep ? max(keep[i], 0) : 0x7fffffff;
+      grow[k] = max(n_new ? n_new[i] : n_new_all, 0);
+      lens[i] = clamp_len(p, p.lens[i]);
+    }
+  }
   __syncthreads();
-  int kept[kRowsPerThread], grow[kRowsPerThread], page[kRowsPerThread];
   int cut_from = 0, cut_to = 0;                           // pages that a row which is its own parent gives up
 #pragma unroll
   for (int k = 0; k < kRowsPerThread; ++k) {
     const int i = tid * rpt + k;
-    const bool there = k < rpt && i < p.batch;
-    kept[k] = grow[k] = 0;
-    page[k] = -1;
     ForkRow f{(uint16_t)i, 0, 0, 0};
     bool changes = false;
-    if (there) {
-      const int from = parent_of(p, parents, i);
-      if (from >= 0) kept[k] = kept_len(lens[from], keep, i);
-      const int g = max(n_new ? n_new[i] : n_new_all, 0);
-      grow[k] = (int64_t)kept[k] + g <= room ? g : 0;
+    if (k < rpt && i < p.batch) {
+      if (from[k] >= 0) kept[k] = min(lens[from[k]], most[k]);
+      if ((int64_t)kept[k] + grow[k] > room) grow[k] = 0;
       // (of the parent's row, which holds the same pages and is not written yet, or of its own)
-      if (grow[k] > 0 && (kept[k] & page_mask)) page[k] = p.table[(int64_t)(kFork ? from : i) * p.stride + (kept[k] >> p.shift)];
-      if (page[k] >= p.n_pages) page[k] = -1;
-      tail[i] = max(page[k], -1);
+      if (grow[k] > 0 && (kept[k] & page_mask)) page[k] = p.table[(int64_t)(kFork ? from[k] : i) * p.stride + (kept[k] >> p.shift)];
       if constexpr (kFork) {
-        f.from = (uint16_t)from;
+        f.from = (uint16_t)from[k];
         f.had = held_pages(lens[i], p.shift);
         f.keeps = held_pages(kept[k], p.shift);
-        changes = from != i && (f.had || f.keeps);
-        if (from == i) { cut_from = f.keeps; cut_to = f.had; }
+        changes = from[k] != i && (f.had || f.keeps);
+        if (from[k] == i) { cut_from = f.keeps; cut_to = f.had; }
       }
     }
     if constexpr (kFork) list_fork(f, changes, forks, &n_forks, &width);   // (a row a thread)
@@ -220,10 +229,27 @@ __global__ __launch_bounds__(kPlanThreads) void pages_grow_kernel(PoolArg p, con
     __syncthreads();
   }
   // counts of the first pages, and of the rows' last ones
-  int holders[kRowsPerThread];
+  int holders[kRowsPerThread], slot[kRowsPerThread];
 #pragma unroll
-  for (int k = 0; k < kRowsPerThread; ++k) holders[k] = page[k] >= 0 ? p.refs[page[k]] : 0;
+  for (int k = 0; k < kRowsPerThread; ++k) {
+    const int i = tid * rpt + k;
+    if (page[k] < 0 || page[k] >= p.n_pages) page[k] = -1;
+    holders[k] = page[k] >= 0 ? p.refs[page[k]] : 0;
+    slot[k] = 0;
+    if (holders[k] > 1) {                                 // (there are more slots than rows)
+      int h = (int)((uint32_t)page[k] * 2654435769u >> 16) & (kSlots - 1);
+      for (;;) {
+        const int held = atomicCAS(&shared_page[h], -1, page[k]);
+        if (held == -1 || held == page[k]) break;
+        h = (h + 1) & (kSlots - 1);
+      }
+      atomicAdd(&writers[h], 1);
+      atomicMax(&last_writer[h], i);
+      slot[k] = h;
+    }
+  }
   uint32_t free_mask = free_pages(p, 0);
+  __syncthreads();
   uint32_t want[kRowsPerThread];
   bool copies[kRowsPerThread];
   Scan3 mine{0u, 0u, (uint32_t)__popc(free_mask)};
@@ -233,15 +259,8 @@ __global__ __launch_bounds__(kPlanThreads) void pages_grow_kernel(PoolArg p, con
     want[k] = 0;
     copies[k] = false;
     if (grow[k] == 0) continue;
-    if (holders[k] > 1) {                                 // rows before this one take copies
-      int earlier = 0, j = 0;
-      for (; j + 4 <= i; j += 4) {
-        const int4 t = *reinterpret_cast<const int4*>(&tail[j]);
-        earlier += (t.x == page[k]) + (t.y == page[k]) + (t.z == page[k]) + (t.w == page[k]);
-      }
-      for (; j < i; ++j) earlier += tail[j] == page[k];
-      copies[k] = earlier < holders[k] - 1;
-    }
+    // rows before this one take copies; if nobody else holds the page, the last of its writers keeps it
+    if (holders[k] > 1) copies[k] = holders[k] > writers[slot[k]] || i != last_writer[slot[k]];
     const int first = copies[k] ? kept[k] >> p.shift : held_pages(kept[k], p.shift);
     first_col[i] = first;
     want[k] = (uint32_t)(held_pages(kept[k] + grow[k], p.shift) - first);
@@ -250,8 +269,9 @@ __global__ __launch_bounds__(kPlanThreads) void pages_grow_kernel(PoolArg p, con
   }
   Scan3 all;
   const Scan3 before = block_scan(mine, sums, &all);
+  const uint32_t asked = all.x, all_copies = all.y;
   // the lowest free pages, as many as are asked for
-  const int need = (int)(all.x < (uint32_t)p.n_pages ? all.x : (uint32_t)p.n_pages);
+  const int need = (int)(asked < (uint32_t)p.n_pages ? asked : (uint32_t)p.n_pages);
   int* list = need <= kListRoom ? list_lds : free_list;
   int found = 0, at = (int)before.z, p0 = 0;
   for (;;) {
@@ -279,29 +299,27 @@ __global__ __launch_bounds__(kPlanThreads) void pages_grow_kernel(PoolArg p, con
   }
   __syncthreads();
   const int last = stop;
-  int granted = 0, copied = 0, move = (int)before.y;
+  int move = (int)before.y;
+  if (tid == 0 && last == p.batch) { n_granted = (int)asked; n_copied = (int)all_copies; }
   b = before.x;
 #pragma unroll
   for (int k = 0; k < kRowsPerThread; ++k) {
     const int i = tid * rpt + k;
-    const uint32_t end = op_add_sat(b, want[k]);
     if (k < rpt && i < p.batch) {
+      if (i == last) { n_granted = (int)b; n_copied = move; }
       if (i >= last && (want[k] > 0 || holders[k] > 1)) grow[k] = 0;
       begin[i] = i < last ? (int)b : 0x7fffffff;
       p.lens[i] = kept[k] + grow[k];
-      if (i < last) granted = (int)end;
       if (i < last && copies[k]) {
         m.src[move] = page[k];
         m.dst[move] = list[b];
         m.rows[move] = kept[k] & page_mask;
         atomicSub(&p.refs[page[k]], 1);
-        copied = ++move;
+        ++move;
       }
     }
-    b = end;
+    b = op_add_sat(b, want[k]);
   }
-  if (granted) atomicMax(&n_granted, granted);
-  if (copied) atomicMax(&n_copied, copied);
   __syncthreads();
   if (tid == 0) *m.count = n_copied;
   // the pages themselves: the q-th belongs to the last row that begins at or before q
