@@ -488,7 +488,7 @@ typedef struct shadowkv_logits {
  *                may overlap need a workspace each.
  * Sums, logarithms and ranks are fp64, the sum of exponentials right to 2^-39 (so that scores of different rows nearer than 2^-37 are
  * not told apart, unless the rows have the same logits); scores are rounded once.  The same call gives the same bits, and rows of equal
- * logits equal sums, whatever their addresses are.
+ * logits equal sums, whatever their addresses are; a row's sum may differ in its last bits with how many rows a call has.
  */
 int shadowkv_beam_select(const shadowkv_logits *logits, const float *scores, const uint8_t *finished, const int32_t *lengths,
                          double length_penalty, double logit_scale, int32_t end_token, int32_t n_out, float *out_scores,
@@ -509,7 +509,8 @@ typedef struct shadowkv_rows {
 /*
  * Replaces row i of every array by what row parents[i] was before the call, in place, in one launch for up to 64 arrays.  Rows with
  * a parent outside [0, n_rows), and those that are their own parent, are left as they are (and not read).
- *   arrays  host [n_arrays], n_arrays in [0, 4096]; an array may not overlap itself, another one of the call, or parents
+ *   arrays  host [n_arrays], n_arrays in [0, 4096]; an array may not overlap itself, another one of the call, or parents (it is refused
+ *           where its first or last piece lies in the other; arrays that only interleave do not overlap)
  *   parents dev [n_rows] int32, n_rows in [0, 2048]
  * Pieces are moved 16 bytes at a time where the address, the strides and `inner` of an array are multiples of 16, else 4 or 1.
  */
@@ -556,7 +557,7 @@ typedef struct shadowkv_page_moves {
  *   moves      out: the copies to be made (rows: tokens that the page holds), before anything is appended; capacity >= batch, no
  *              member NULL
  *   workspace  dev >= shadowkv_pages_workspace_bytes(), 256-byte aligned, contents do not matter, one for each call that may overlap
- * parents, keep_lens and n_new may not share memory with the pool.
+ * parents, keep_lens and n_new may not share memory with what is written, nor the pool, moves and the workspace with each other.
  */
 int shadowkv_pages_update(const shadowkv_page_pool *pool, const int32_t *parents, const int32_t *keep_lens, const int32_t *n_new,
                           int32_t n_new_all, const shadowkv_page_moves *moves, void *workspace, size_t workspace_bytes, void *stream);

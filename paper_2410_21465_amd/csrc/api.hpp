@@ -44,4 +44,14 @@ inline int check_workspace(void* ws, size_t have, size_t need) {
   return SHADOWKV_OK;
 }
 
+// memory that an argument covers (p may be NULL: none)
+struct Bytes {
+  const void* p;
+  size_t n;
+};
+inline bool meet(const Bytes& a, const Bytes& b) {
+  const char *x = static_cast<const char*>(a.p), *y = static_cast<const char*>(b.p);
+  return x && y && a.n && b.n && x < y + b.n && y < x + a.n;
+}
+
 }  // namespace skv

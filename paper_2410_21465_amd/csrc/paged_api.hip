@@ -257,6 +257,13 @@ PoolArg pool_arg(const shadowkv_page_pool* p) {
 }
 MovesArg moves_arg(const shadowkv_page_moves* m) { return {m->src, m->dst, m->rows, m->count, m->capacity}; }
 
+bool overlap(const Bytes* of, int n) {
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < i; ++j)
+      if (meet(of[i], of[j])) return true;
+  return false;
+}
+
 size_t pages_workspace(const shadowkv_page_pool* p) { return kAlign + up((size_t)p->n_pages * sizeof(int32_t)); }
 
 // a cache whose pages alone matter
@@ -290,6 +297,15 @@ int shadowkv_pages_update(const shadowkv_page_pool* pool, const int32_t* parents
   if (n_new_all < 0) return fail_inval("n_new_all must be >= 0");
   rc = check_workspace(workspace, workspace_bytes, pages_workspace(pool));
   if (rc != SHADOWKV_OK) return rc;
+  const size_t b = (size_t)pool->batch * sizeof(int32_t);
+  const Bytes ins[3] = {{parents, b}, {keep_lens, b}, {n_new, b}};
+  const Bytes outs[8] = {{pool->page_table, ((size_t)(pool->batch - 1) * pool->table_stride + pool->pages_per_seq) * sizeof(int32_t)}, {pool->kv_lens, b},
+                         {pool->page_refs, (size_t)pool->n_pages * sizeof(int32_t)}, {workspace, pages_workspace(pool)}, {moves->src, b}, {moves->dst, b},
+                         {moves->rows, b}, {moves->count, sizeof(int32_t)}};
+  for (const Bytes& o : outs)
+    for (const Bytes& i : ins)
+      if (meet(o, i)) return fail_inval("parents, keep_lens or n_new share memory with what is written");
+  if (overlap(outs, 8)) return fail_inval("the pool, moves and the workspace share memory");
   const hipError_t e = launch_pages_update(pool_arg(pool), parents, keep_lens, n_new, n_new_all, moves_arg(moves),
                                            reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kAlign), static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SHADOWKV_OK : fail_hip("pages update", e);
@@ -304,6 +320,11 @@ int shadowkv_pages_compact(const shadowkv_page_pool* pool, int32_t max_moves, co
   if (max_moves < 0) return fail_inval("max_moves must be >= 0");
   rc = check_workspace(workspace, workspace_bytes, pages_workspace(pool));
   if (rc != SHADOWKV_OK) return rc;
+  const size_t b = (size_t)pool->batch * sizeof(int32_t), c = (size_t)moves->capacity * sizeof(int32_t);
+  const Bytes outs[9] = {{pool->page_table, ((size_t)(pool->batch - 1) * pool->table_stride + pool->pages_per_seq) * sizeof(int32_t)}, {pool->kv_lens, b},
+                         {pool->page_refs, (size_t)pool->n_pages * sizeof(int32_t)}, {workspace, pages_workspace(pool)}, {moves->src, c}, {moves->dst, c},
+                         {moves->rows, c}, {moves->count, sizeof(int32_t)}, {n_used, sizeof(int32_t)}};
+  if (overlap(outs, 9)) return fail_inval("the pool, moves, n_used and the workspace share memory");
   int32_t* ws = static_cast<int32_t*>(workspace);
   const hipError_t e = launch_pages_compact(pool_arg(pool), max_moves, moves_arg(moves), n_used, ws + kAlign / sizeof(int32_t), ws,
                                             static_cast<hipStream_t>(stream));

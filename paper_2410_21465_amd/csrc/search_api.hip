@@ -34,12 +34,6 @@ int check_logits(const shadowkv_logits* x, int n_out, bool pointers) {
   return SHADOWKV_OK;
 }
 
-struct Span {
-  const char* p;
-  size_t n;
-};
-bool meet(const Span& a, const Span& b) { return a.p && b.p && a.n && b.n && a.p < b.p + b.n && b.p < a.p + a.n; }
-
 struct BeamLayout {
   int part_len, n_parts, n_blocks;
   size_t peaks, offers, total;
@@ -100,10 +94,9 @@ int shadowkv_beam_select(const shadowkv_logits* logits, const float* scores, con
   const int eb = logit_bytes(logits->dtype);
   const size_t span = ((logits->n_groups > 1 ? (size_t)(logits->n_groups - 1) * logits->group_stride : 0) +
                        (logits->n_beams > 1 ? (size_t)(logits->n_beams - 1) * logits->beam_stride : 0) + logits->vocab) * eb;
-  auto at = [](const void* p, size_t n) { return Span{static_cast<const char*>(p), n}; };
-  const Span ins[4] = {at(scores, in * 4), at(finished, in), at(lengths, in * 4), at(logits->data, span)};
-  const Span outs[6] = {at(out_scores, out * 4), at(out_finished, out), at(out_lengths, out * 4), at(out_parents, out * 4), at(out_tokens, out * 4),
-                        at(workspace, workspace_bytes)};
+  const Bytes ins[4] = {{scores, in * 4}, {finished, in}, {lengths, in * 4}, {logits->data, span}};
+  const Bytes outs[6] = {{out_scores, out * 4}, {out_finished, out}, {out_lengths, out * 4}, {out_parents, out * 4}, {out_tokens, out * 4},
+                         {workspace, workspace_bytes}};
   for (int i = 0; i < 6; ++i) {
     for (int j = 0; j < 4; ++j)
       if (meet(outs[i], ins[j]) && !(i == j && i < 3 && n_out == logits->n_beams && outs[i].p == ins[j].p))
@@ -151,8 +144,9 @@ int shadowkv_reorder_rows(const shadowkv_rows* arrays, int32_t n_arrays, const i
       return fail_inval("array %d: the strides span more than 2^48 bytes", k);
     const int64_t low = p.st[1] * (p.sz[1] - 1) + p.inner;   // of all that the narrower stride runs over
     if ((p.sz[1] > 1 && p.st[1] < p.inner) || (p.sz[0] > 1 && p.st[0] < low)) return fail_inval("array %d is written and overlaps itself", k);
-    const Span whole{p.p, (size_t)(p.last + p.inner)}, par{reinterpret_cast<const char*>(parents), (size_t)n_rows * sizeof(int32_t)};
-    if (meet(whole, par) && (p.holds(par.p) || p.holds(par.p + par.n - 1))) return fail_inval("array %d shares memory with parents", k);
+    const char* par = reinterpret_cast<const char*>(parents);
+    const size_t par_bytes = (size_t)n_rows * sizeof(int32_t);
+    if (meet({p.p, (size_t)(p.last + p.inner)}, {par, par_bytes}) && (p.holds(par) || p.holds(par + par_bytes - 1))) return fail_inval("array %d shares memory with parents", k);
     for (int j = 0; j < k; ++j) {
       const shadowkv_rows& b = arrays[j];
       if (b.n_outer == 0 || b.inner == 0) continue;

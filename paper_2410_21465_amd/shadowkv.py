@@ -638,6 +638,8 @@ class _OnCurrent:
 
 def _launch(device: torch.device, stream):
     """``_Launch``, or without its costs where the current device and its current stream are meant."""
+    if device.type != "cuda":
+        raise ValueError(f"the tensors must be on the GPU, not {device}")
     index = device.index
     if stream is None and index is not None and index == torch._C._cuda_getDevice():
         return _OnCurrent(torch._C._cuda_getCurrentRawStream(index))
@@ -772,6 +774,7 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, kv_lens: torch.Tensor, s
 
 # ---- a search over several continuations: the choice over beams and vocabulary, and the state that follows it ----
 
+_INT32 = 2 ** 31 - 1       # (ctypes cuts longer numbers off without a word)
 _LOGITS = {torch.bfloat16: LOGITS_BF16, torch.float16: LOGITS_FP16, torch.float32: LOGITS_FP32}
 
 
@@ -800,9 +803,11 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n_out: int = 0, fini
     if lengths is not None:
         _want(lengths, "lengths", torch.int32, rows, dev)
         kinds.append(("lengths", torch.int32))
+    if vocab > _INT32 or groups > _INT32 or abs(end_token) > _INT32:
+        raise ValueError("sizes and end_token must fit 32 bits")
     c = C.byref(CLogits(logits.data_ptr(), sg, sb, groups, beams, vocab, _LOGITS[logits.dtype]))
     L = lib()
-    need = L.shadowkv_beam_select_workspace_bytes(c, n)
+    need = L.shadowkv_beam_select_workspace_bytes(c, n if 0 < n <= 64 else 0)
     if need == 0:
         raise ShadowKVError(EINVAL, last_error())
     with _launch(dev, stream) as st:
@@ -889,6 +894,8 @@ def pages_copy(caches, src: torch.Tensor, dst: torch.Tensor, rows: Optional[torc
     _want(dst, "dst", torch.int32, src.shape, dev)
     if rows is not None:
         _want(rows, "rows", torch.int32, src.shape, dev)
+    if src.numel() > _INT32:
+        raise ValueError("more than 2^31 - 1 pages")
     if any(c.device != dev for c in caches) or any(c.device != dev for c in to):
         raise ValueError(f"the caches must be on {dev}")
     with _launch(dev, stream) as st:
@@ -904,6 +911,8 @@ class PagePool:
     have been copied."""
 
     def __init__(self, batch: int, pages_per_seq: int, n_pages: int, page_size: int, device="cuda"):
+        if max(batch, pages_per_seq, n_pages, page_size) > _INT32:
+            raise ValueError("sizes must fit 32 bits")
         c = CPagePool(None, pages_per_seq, None, None, batch, pages_per_seq, n_pages, page_size)
         need = int(lib().shadowkv_pages_workspace_bytes(C.byref(c)))
         if need == 0:
@@ -940,6 +949,8 @@ class PagePool:
         ``paged_append`` wants it; a row that the pages do not suffice for gets none.  Copies, in every cache of ``caches``, the last pages that
         rows share and are about to write."""
         each = isinstance(n_new, torch.Tensor)
+        if not each and not 0 <= n_new <= _INT32:
+            raise ValueError(f"n_new must be in [0, 2^31), not {n_new}")
         for name, t in (("parents", parents), ("keep_lens", keep_lens), ("n_new", n_new if each else None)):
             if t is not None:
                 if t.numel() != self.batch:
@@ -957,6 +968,8 @@ class PagePool:
         """Moves the highest used pages into the lowest free ones (at most ``max_moves``), in every cache of ``caches``.  Returns ``n_used [1]``
         int32 on the device: all pages from there on are free."""
         room, caches = self.move_src.numel(), self._layers(caches)
+        if max_moves is not None and not 0 <= max_moves <= _INT32:
+            raise ValueError(f"max_moves must be in [0, 2^31), not {max_moves}")
         with _launch(self.device, stream) as st:
             _check(lib().shadowkv_pages_compact(self._c, room if max_moves is None else int(max_moves), self._compact_moves, self.n_used.data_ptr(),
                                                 self.workspace.data_ptr(), self.workspace.numel(), st))

@@ -97,6 +97,31 @@ def test_masks_of_the_lowest_value():
         both(x, s, 6, logit_scale=0.5)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_logits_too_small_to_be_normal(dtype):
+    x = torch.zeros(1, 3, 4000, device="cuda").to(LOGIT_TYPES[dtype])
+    bits = x.view(torch.int32 if dtype == "fp32" else torch.int16)
+    bits[0, 0, 100:105] = torch.tensor([1, 3, 2, 3, 5], device="cuda").to(bits.dtype)
+    bits[0, 1, 7] = 4
+    x[0, 2] = -1.0
+    got = both(x, torch.tensor([[0.0, -1.0, -2.0]], device="cuda"), 7)
+    assert got["tokens"][0].tolist() == [104, 101, 103, 102, 100, 0, 1]
+
+
+def test_a_temperature_that_leaves_nothing_but_ties():
+    x, _, _ = draw(2, 3, 999, "fp32", 19)
+    both(x, torch.zeros(2, 3, device="cuda"), 6, logit_scale=1e-30)
+
+
+def test_how_many_rows_a_call_has_changes_its_sums_in_their_last_bits_only():
+    x, s, _ = draw(40, 4, 70000, "bf16", 20)
+    all_of_them = S.beam_select(x, s, n_out=4)
+    for g in (0, 39):
+        one = S.beam_select(x[g:g + 1], s[g:g + 1], n_out=4)
+        assert torch.equal(one["tokens"][0], all_of_them["tokens"][g]) and torch.equal(one["parents"][0] + 4 * g, all_of_them["parents"][g])
+        assert ((one["scores"][0] - all_of_them["scores"][g]).abs() <= 2.0 ** -23 * one["scores"][0].abs()).all()
+
+
 def test_logits_far_apart():
     x, s, _ = draw(1, 5, 7000, "fp32", 13)
     x[0, 0, 3000:] += 2e4                                            # a part far above those before it
@@ -140,8 +165,11 @@ def test_outputs_in_place_of_inputs():
     assert got is out and all(torch.equal(got[k], want[k]) for k in want)
     with pytest.raises(ValueError):
         S.beam_select(x, s, finished=done, out={"scores": s})
-    with pytest.raises(S.ShadowKVError):
-        S.beam_select(x, s, n_out=65)
+    for n in (65, -1, 2 ** 32 + 3):
+        with pytest.raises(S.ShadowKVError):
+            S.beam_select(x, s, n_out=n)
+    with pytest.raises(ValueError):
+        S.beam_select(x, s, end_token=2 ** 32)
     assert S.beam_select(x[:0], s[:0])["tokens"].shape == (0, 6)
 
 

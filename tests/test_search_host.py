@@ -80,11 +80,11 @@ def test_reorder_refusals():
 
 
 def pool(**kw):
-    return make(S.CPagePool, dict(page_table=FAKE, table_stride=10, kv_lens=FAKE, page_refs=FAKE, batch=3, pages_per_seq=10, n_pages=50, page_size=16), kw)
+    return make(S.CPagePool, dict(page_table=7 * FAR, table_stride=10, kv_lens=8 * FAR, page_refs=9 * FAR, batch=3, pages_per_seq=10, n_pages=50, page_size=16), kw)
 
 
 def moves(**kw):
-    return make(S.CPageMoves, dict(src=FAKE, dst=FAKE, rows=FAKE, count=FAKE, capacity=3, reserved=0), kw)
+    return make(S.CPageMoves, dict(src=10 * FAR, dst=11 * FAR, rows=12 * FAR, count=13 * FAR, capacity=3, reserved=0), kw)
 
 
 def update(p=None, m=None, grow=1, ws=FAKE, room=1 << 20):
@@ -118,6 +118,17 @@ def test_update_and_compact_refusals():
     for call in (update, compact):
         assert call(ws=None) == S.EWORKSPACE and call(ws=FAKE + 8) == S.EWORKSPACE and call(room=need - 1) == S.EWORKSPACE
     assert S.lib().shadowkv_pages_workspace_bytes(C.byref(pool(batch=0))) == 0
+    # arguments that share memory
+    for where in (7 * FAR, 8 * FAR + 8, 9 * FAR + 196, 10 * FAR, 13 * FAR - 4, FAKE):
+        for place in range(3):
+            args = [None] * 3
+            args[place] = where
+            p, m = pool(), moves()
+            assert S.lib().shadowkv_pages_update(C.byref(p), *args, 0, C.byref(m), FAKE, 1 << 20, None) == S.EINVAL and "share" in S.last_error()
+    for bad in (dict(src=11 * FAR), dict(rows=9 * FAR), dict(count=8 * FAR + 4), dict(dst=7 * FAR + 100)):
+        assert update(m=moves(**bad)) == S.EINVAL and "share" in S.last_error()
+        assert compact(m=moves(**bad)) == S.EINVAL and "share" in S.last_error()
+    assert update(pool(kv_lens=9 * FAR)) == S.EINVAL and compact(pool(page_table=FAKE)) == S.EINVAL
 
 
 def cache(**kw):
@@ -153,7 +164,17 @@ def test_python_refuses_what_is_not_on_the_gpu_or_of_another_shape():
         S.pages_copy([], torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int32))
     with pytest.raises(S.ShadowKVError):
         S.PagePool(0, 4, 16, 16, device="cpu")
+    with pytest.raises(ValueError):
+        S.PagePool(2 ** 32 + 2, 4, 16, 16, device="cpu")
     p = S.PagePool(2, 4, 16, 16, device="cpu")
+    for call in (p.update, p.compact):
+        with pytest.raises(ValueError):
+            call()
+    for bad in (-1, 2 ** 32):
+        with pytest.raises(ValueError):
+            p.update(n_new=bad)
+        with pytest.raises(ValueError):
+            p.compact(max_moves=bad)
     with pytest.raises(ValueError):
         p.update(n_new=torch.zeros(3, dtype=torch.int32))
     with pytest.raises(ValueError):
