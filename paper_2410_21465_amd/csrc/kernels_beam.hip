@@ -265,15 +265,16 @@ __device__ __forceinline__ int sort_room(JoinRoom<T>& room, int n, int tid) {
     const uint32_t item = room.item[i];
     int rank = 0;
     for (int j = 0; j < c; j += 8) {
+      uint32_t items[8];
+      if constexpr (kTies) {                              // (asked for with the keys, not where one is equal: each is to itself)
+        *reinterpret_cast<uint4*>(items) = *reinterpret_cast<const uint4*>(&room.item[j]);
+        *reinterpret_cast<uint4*>(items + 4) = *reinterpret_cast<const uint4*>(&room.item[j + 4]);
+      }
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
         const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&room.key[j + e]);
-        rank += o.x > k;
-        rank += o.y > k;
-        if constexpr (kTies) {
-          rank += o.x == k && room.item[j + e] < item;
-          rank += o.y == k && room.item[j + e + 1] < item;
-        }
+        rank += (int)(o.x > k) + (int)(o.y > k);
+        if constexpr (kTies) rank += ((int)(o.x == k) & (int)(items[e] < item)) + ((int)(o.y == k) & (int)(items[e + 1] < item));
       }
     }
     if (rank < n) { room.best[rank] = k; room.best_item[rank] = item; }
