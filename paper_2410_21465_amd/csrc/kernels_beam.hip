@@ -340,7 +340,9 @@ __device__ __forceinline__ void take_exactly(Key key, int n_entries, int n, uint
   };
   for (int b = 63; b >= 0; --b) {
     const uint64_t up = (bound >> b | 1ull) << b;         // (bits above b are right; where bit b is set already this is not more)
-    if (up > bound && count(up - 1, 0) >= n) bound = up;
+    const int reach = up > bound ? count(up - 1, 0) : 0;
+    if (reach >= n) bound = up;
+    if (reach == n) break;
   }
   uint32_t below = ~0u;
   if constexpr (kTies) {                                  // the most numbers that do not make n yet, and one more
@@ -428,28 +430,33 @@ __device__ __forceinline__ void row_offers(const BeamArgs& a, int row, JoinRoom<
       const uint32_t* peak = a.peaks + (int64_t)row * a.n_blocks;
       const int n_best = top_items<false>([&](int i, uint32_t&) { return key_of(peak[i], i); }, a.n_blocks, a.n, room, tid);
       auto block = [&](int i) { return (int)~(uint32_t)room.best[i]; };
-      // tokens of those blocks that are not less than the n-th block's largest
-      const uint64_t bound = n_best == a.n ? room.best[n_best - 1] >> 32 << 32 : 1;
+      auto each_token = [&](auto f) {
+        for (int i0 = 0; i0 < n_best; i0 += kAtOnce) {
+          const int i = i0 + tid / kLanes;
+          const int at = i < n_best ? block(i) * kBlock + tid % kLanes * kEach : a.vocab;
+          float x[kEach];
+          if (at + kEach <= a.vocab) {
+            uint32_t raw[kEach * EB / 4];
+            __builtin_memcpy(raw, p + (int64_t)at * EB, kEach * EB);
+            Logit<DT>::template unpack<kEach>(raw, x);
+          } else {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) x[e] = at + e < a.vocab ? Logit<DT>::one(p + (int64_t)(at + e) * EB) : -INFINITY;
+          }
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) f(key_of(f32_key(x[e]), at + e));
+        }
+      };
+      // tokens that are not less than the n-th block's largest (where fewer blocks hold any: than the n-th of the threads' largest)
+      uint64_t bound = n_best == a.n ? room.best[n_best - 1] >> 32 << 32 : 0;
+      if (bound == 0) {
+        uint64_t mine = 0;
+        each_token([&](uint64_t k) { mine = k > mine ? k : mine; });
+        bound = find_bound(mine, a.n, room, tid);
+      }
       if (tid == 0) room.count = 0;
       team_sync<T>();
-      for (int i0 = 0; i0 < n_best; i0 += kAtOnce) {
-        const int i = i0 + tid / kLanes;
-        const int at = i < n_best ? block(i) * kBlock + tid % kLanes * kEach : a.vocab;
-        float x[kEach];
-        if (at + kEach <= a.vocab) {
-          uint32_t raw[kEach * EB / 4];
-          __builtin_memcpy(raw, p + (int64_t)at * EB, kEach * EB);
-          Logit<DT>::template unpack<kEach>(raw, x);
-        } else {
-#pragma unroll
-          for (int e = 0; e < kEach; ++e) x[e] = at + e < a.vocab ? Logit<DT>::one(p + (int64_t)(at + e) * EB) : -INFINITY;
-        }
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-          const uint64_t k = key_of(f32_key(x[e]), at + e);
-          take(k, 0, k >= bound, room, lane);
-        }
-      }
+      each_token([&](uint64_t k) { take(k, 0, k >= bound, room, lane); });
       team_sync<T>();
       if (__builtin_expect(room.count > JoinRoom<T>::kRoom, 0))
         take_exactly<false>([&](int i, uint32_t& item) -> uint64_t {
@@ -468,21 +475,15 @@ __device__ __forceinline__ void row_offers(const BeamArgs& a, int row, JoinRoom<
   if (tid >= count && tid < a.n) offer[tid] = BeamOffer{0, -INFINITY, -1};
 }
 
-// of what the rows of a group offer, the best
-template <int T>
-__device__ __forceinline__ void choose(const BeamArgs& a, int group, const BeamOffer* all, JoinRoom<T>& room, int tid) {
-  const int found = top_items<true>([&](int i, uint32_t& item) -> uint64_t {
-    item = (uint32_t)i;                                   // in order of rows, then of places
-    return all[i].rank;
-  }, a.beams * a.n, a.n, room, tid);
-  // (all that this group's rows held has been read before anything is written: the outputs may be the inputs)
+// place `tid` of a group's choice: offer `item`, if there is one.  (By one wave, so that all that the group's rows held has been read before anything is
+// written: the outputs may be the inputs.)
+__device__ __forceinline__ void give_out(const BeamArgs& a, int group, const BeamOffer* all, bool there, int item, int tid) {
   float out_s = -INFINITY;
   int parent = -1, token = -1, length = 0;
   bool ended = false;
-  if (tid < found) {
-    const int i = (int)room.best_item[tid];
-    const BeamOffer o = all[i];
-    parent = group * a.beams + i / a.n;
+  if (there) {
+    const BeamOffer o = all[item];
+    parent = group * a.beams + item / a.n;
     const bool was = a.finished && a.finished[parent];
     out_s = o.score;
     token = o.token;
@@ -500,6 +501,16 @@ __device__ __forceinline__ void choose(const BeamArgs& a, int group, const BeamO
   }
 }
 
+// of what the rows of a group offer, the best
+template <int T>
+__device__ __forceinline__ void choose(const BeamArgs& a, int group, const BeamOffer* all, JoinRoom<T>& room, int tid) {
+  const int found = top_items<true>([&](int i, uint32_t& item) -> uint64_t {
+    item = (uint32_t)i;                                   // in order of rows, then of places
+    return all[i].rank;
+  }, a.beams * a.n, a.n, room, tid);
+  give_out(a, group, all, tid < found, tid < found ? (int)room.best_item[tid] : 0, tid);
+}
+
 template <int DT>
 __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
   __shared__ JoinRoom<kJoinThreads> room;
@@ -509,18 +520,130 @@ __global__ __launch_bounds__(kJoinThreads) void beam_choose_kernel(BeamArgs a) {
   __shared__ JoinRoom<kJoinThreads> room;
   choose(a, blockIdx.x, a.offers + (int64_t)blockIdx.x * a.beams * a.n, room, threadIdx.x);
 }
-// both in one launch, a wave for each of a group's rows: where there is little to look through a launch less counts for more than three waves less
-// a row.  A call at 1 x 4 x 32000, 4 / 8 / 16 places: 15.2 / 15.8 / 20.3 us, 17.5 apart; 16 x 4 x 50257, 4 places: 18.2 and 17.6;
-// 64 x 8 x 8000, 8 places: 18.6 and 17.8.
+// ---- small calls: both in one launch, two waves for each of a group's rows -----------------------------------------------------
+// Where there is little to look through a launch less counts for more than fewer waves a row.  One wave of a row finds its best tokens, the other
+// its sum.  Few places out of few keys are taken one by one, without LDS: the largest of the wave, n times.
 constexpr int kFewBeams = 4, kFewInOne = 8, kFewBlocks = 128;
+struct Taken {
+  uint64_t key;                                           // lane i: the i-th largest, 0 if there are fewer
+  int lane;                                               // whose it was
+};
+// equal keys go in order of lanes
+template <int K>
+__device__ __forceinline__ Taken take_in_turn(uint64_t (&k)[K], int n, int lane) {
+  Taken t{0, 0};
+  for (int i = 0; i < n; ++i) {
+    uint64_t mine = k[0];
+#pragma unroll
+    for (int e = 1; e < K; ++e) mine = k[e] > mine ? k[e] : mine;
+    const uint32_t upper = wave_max_u32((uint32_t)(mine >> 32));
+    const uint32_t lower = wave_max_u32((uint32_t)(mine >> 32) == upper ? (uint32_t)mine : 0u);
+    const uint64_t top = (uint64_t)upper << 32 | lower;
+    if (top == 0) break;
+    const int from = __ffsll((unsigned long long)__ballot(mine == top)) - 1;
+    bool here = lane == from;
+#pragma unroll
+    for (int e = 0; e < K; ++e)
+      if (here && k[e] == top) { k[e] = 0; here = false; }
+    if (lane == i) t = Taken{top, from};
+  }
+  return t;
+}
+
 template <int DT>
-__global__ __launch_bounds__(kFewBeams * kWave) void beam_finish_kernel(BeamArgs a) {
+__global__ __launch_bounds__(2 * kFewBeams * kWave) void beam_finish_kernel(BeamArgs a) {
+  constexpr int EB = Logit<DT>::bytes, kEach = 8, kLanes = kBlock / kEach, kAtOnce = kWave / kLanes, kBatch = kFewInOne / kAtOnce;
   __shared__ JoinRoom<kWave> rooms[kFewBeams];
   __shared__ BeamOffer offers[kFewBeams * kFewInOne];
-  const int b = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & (kWave - 1);
-  row_offers<DT>(a, blockIdx.x * a.beams + b, rooms[b], offers + b * a.n, lane);
+  __shared__ RowSum sums[kFewBeams];
+  const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & (kWave - 1), group = blockIdx.x;
+  const int b = w < a.beams ? w : w - a.beams, row = group * a.beams + b;
+  const float s = a.scores[row];
+  const bool lives = row_lives(s), done = a.finished && a.finished[row];
+  JoinRoom<kWave>& room = rooms[b];
+  uint64_t best = 0;                                      // lane i: (logit, ~token) of the row's i-th best
+  int count = 0;
+  if (w >= a.beams) {
+    const RowSum sum = lives && !done ? row_sum(a, row, lane) : RowSum{0.0, -INFINITY};
+    if (lane == 0) sums[b] = sum;
+  } else if (lives && !done) {
+    const uint8_t* p = a.logits + (int64_t)group * a.group_stride + (int64_t)b * a.beam_stride;
+    const uint32_t* peak = a.peaks + (int64_t)row * a.n_blocks;
+    auto key_of = [](uint32_t upper, int number) -> uint64_t { return upper > kLowestKey ? ((uint64_t)upper << 32) | (uint32_t)~number : 0; };
+    uint64_t k[kFewBlocks / kWave];
+#pragma unroll
+    for (int e = 0; e < kFewBlocks / kWave; ++e) {
+      const int i = e * kWave + lane;
+      k[e] = i < a.n_blocks ? key_of(peak[i], i) : 0;
+    }
+    const Taken blocks = take_in_turn(k, a.n, lane);
+    const int n_best = __popcll(__ballot(blocks.key != 0));
+    if (a.vocab >= kEach) {
+      uint32_t raw[kBatch][kEach * EB / 4];
+      int at[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int i = j * kAtOnce + lane / kLanes;
+        const int block = (int)~(uint32_t)__shfl((int)(uint32_t)blocks.key, i, kWave);
+        at[j] = i < n_best ? block * kBlock + lane % kLanes * kEach : a.vocab;
+        __builtin_memcpy(raw[j], p + (int64_t)min(at[j], a.vocab - kEach) * EB, kEach * EB);
+      }
+      // (a lane at the row's end reads its last tokens, and leaves out what is another's)
+      auto each_token = [&](auto f) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          float x[kEach];
+          Logit<DT>::template unpack<kEach>(raw[j], x);
+          const int first = min(at[j], a.vocab - kEach);
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) f(first + e >= at[j] ? key_of(f32_key(x[e]), first + e) : 0);
+        }
+      };
+      // tokens that are not less than the n-th block's largest (where fewer blocks hold any: than the n-th of the lanes' largest)
+      uint64_t bound = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(blocks.key >> 32), a.n - 1) << 32;
+      if (n_best < a.n) {
+        uint64_t mine = 0;
+        each_token([&](uint64_t key) { mine = key > mine ? key : mine; });
+        bound = find_bound(mine, a.n, room, lane);
+      }
+      if (lane == 0) room.count = 0;
+      team_sync<kWave>();
+      each_token([&](uint64_t key) { take(key, 0, key >= bound, room, lane); });
+      team_sync<kWave>();
+      if (__builtin_expect(room.count > JoinRoom<kWave>::kRoom, 0))
+        take_exactly<false>([&](int i, uint32_t&) -> uint64_t {
+          const int t = (int)~(uint32_t)__shfl((int)(uint32_t)blocks.key, i / kBlock, kWave) * kBlock + i % kBlock;
+          return t < a.vocab ? key_of(f32_key(Logit<DT>::one(p + (int64_t)t * EB)), t) : 0;
+        }, n_best * kBlock, a.n, bound, room, lane);
+      count = min(room.count, JoinRoom<kWave>::kRoom);
+      uint64_t held[JoinRoom<kWave>::kRoom / kWave];
+#pragma unroll
+      for (int e = 0; e < JoinRoom<kWave>::kRoom / kWave; ++e) held[e] = e * kWave + lane < count ? room.key[e * kWave + lane] : 0;
+      best = take_in_turn(held, a.n, lane).key;
+    } else {
+      count = top_items<false>([&](int t, uint32_t&) { return key_of(f32_key(Logit<DT>::one(p + (int64_t)t * EB)), t); }, a.vocab, a.n, room, lane);
+      best = lane < count ? room.best[lane] : 0;
+    }
+  }
   __syncthreads();
-  if (b == 0) choose(a, blockIdx.x, offers, rooms[0], lane);
+  if (w < a.beams && lane < a.n) {
+    BeamOffer o{0, -INFINITY, -1};
+    double weight = 1.0;
+    if (a.penalty != 0.0) weight = pow(fmax((double)a.lengths[row] + (done ? 0.0 : 1.0), 1.0), a.penalty);
+    if (lives && done) {
+      if (lane == 0) o = BeamOffer{f64_key((double)s / weight), s, a.end_token};
+    } else if (best != 0 && sums[b].ref > -INFINITY) {
+      const double score = (double)s - sums[b].log_sum + a.scale * ((double)key_f32((uint32_t)(best >> 32)) - (double)sums[b].ref);
+      o = BeamOffer{f64_key(score / weight), (float)score, (int32_t)~(uint32_t)best};
+    }
+    offers[b * a.n + lane] = o;
+  }
+  __syncthreads();
+  if (w) return;
+  static_assert(kFewBeams * kFewInOne <= kWave, "an offer a lane");
+  uint64_t k[1] = {lane < a.beams * a.n ? offers[lane].rank : 0};
+  const Taken t = take_in_turn(k, a.n, lane);
+  give_out(a, group, offers, t.key != 0, t.lane, lane);
 }
 
 template <int DT>
@@ -530,7 +653,7 @@ hipError_t launch(const BeamArgs& a, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.beams <= kFewBeams && a.n <= kFewInOne && a.n_blocks <= kFewBlocks) {
-    beam_finish_kernel<DT><<<dim3((unsigned)a.groups), a.beams * kWave, 0, st>>>(a);
+    beam_finish_kernel<DT><<<dim3((unsigned)a.groups), 2 * a.beams * kWave, 0, st>>>(a);
     return hipGetLastError();
   }
   beam_join_kernel<DT><<<dim3((unsigned)rows), kJoinThreads, 0, st>>>(a);

@@ -87,6 +87,18 @@ def test_infinite_parts_beside_finite_ones():
     both(x, s, 16)
 
 
+@pytest.mark.parametrize("groups,beams,n", [(2, 3, 6), (1, 6, 20)])
+def test_masks_that_leave_few_blocks(groups, beams, n):
+    """All that is left of a row lies side by side: fewer stretches of it than places, each of them full."""
+    x, s, _ = draw(groups, beams, 30000, "bf16", 21)
+    x[..., :7000], x[..., 7900:] = -math.inf, -math.inf
+    both(x, s, n)
+    x[0, 0, 7001:], x[0, 1, :7899] = -math.inf, -math.inf
+    both(x, s, n)
+    x[0, 2, 7000:7900] = 1.0
+    both(x, s, n)
+
+
 def test_masks_of_the_lowest_value():
     for dtype in ("bf16", "fp16", "fp32"):
         x, s, _ = draw(2, 4, 5000, dtype, 12)
