@@ -521,9 +521,10 @@ __global__ __launch_bounds__(kJoinThreads) void beam_choose_kernel(BeamArgs a) {
   choose(a, blockIdx.x, a.offers + (int64_t)blockIdx.x * a.beams * a.n, room, threadIdx.x);
 }
 // ---- small calls: both in one launch, two waves for each of a group's rows -----------------------------------------------------
-// Where there is little to look through a launch less counts for more than fewer waves a row.  One wave of a row finds its best tokens, the other
-// its sum.  Few places out of few keys are taken one by one, without LDS: the largest of the wave, n times.
-constexpr int kFewBeams = 4, kFewInOne = 8, kFewBlocks = 128;
+// One wave of a row finds its best tokens, the other its sum.  Few places out of few keys are taken one by one, without LDS: the largest of the
+// wave, n times, 0.6 us a place; a third launch costs 2.5 us on the host and 2 on the GPU.  Captured and replayed, rows of 32000: 10.8 us at 1 x 4 with 4
+// places and 13.2 in three launches, 11.6 and 15.5 at 64 x 2 with 2, but 14.7 and 13.1 at 1 x 4 with 8; a row at a time of 1000, 7.8 and 12.1.
+constexpr int kFewBeams = 4, kFewInOne = 4, kFewBlocks = 128;
 struct Taken {
   uint64_t key;                                           // lane i: the i-th largest, 0 if there are fewer
   int lane;                                               // whose it was

@@ -51,6 +51,8 @@ def test_ties_go_to_the_lower_row_and_token(dtype):
     x, s = row.expand(2, 8, 3001).contiguous(), torch.zeros(2, 8, device="cuda")
     both(x, s, 64)
     both(torch.zeros_like(x), s, 64)
+    both(x[:, :4], s[:, :4].contiguous(), 4)
+    both(torch.zeros_like(x)[:, :4], s[:, :4].contiguous(), 4)
     s[:, 3] = 1.0
     both(x, s, 13)
     assert both(torch.full_like(x, -0.0), s, 5)["tokens"][0].tolist() == [0, 1, 2, 3, 4]
@@ -59,7 +61,7 @@ def test_ties_go_to_the_lower_row_and_token(dtype):
     assert both(mixed, s, 5)["tokens"][0].tolist() == [0, 1, 2, 3, 4]
 
 
-@pytest.mark.parametrize("n", [1, 8, 64])
+@pytest.mark.parametrize("n", [1, 4, 8, 64])
 def test_sorted_rows(n):
     up = torch.arange(20000, device="cuda", dtype=torch.float32) * 1e-3
     x = torch.stack([up, up.flip(0), up.roll(9999)])[None]
@@ -87,7 +89,7 @@ def test_infinite_parts_beside_finite_ones():
     both(x, s, 16)
 
 
-@pytest.mark.parametrize("groups,beams,n", [(2, 3, 6), (1, 6, 20)])
+@pytest.mark.parametrize("groups,beams,n", [(2, 3, 4), (2, 3, 6), (1, 6, 20)])
 def test_masks_that_leave_few_blocks(groups, beams, n):
     """All that is left of a row lies side by side: fewer stretches of it than places, each of them full."""
     x, s, _ = draw(groups, beams, 30000, "bf16", 21)
@@ -106,6 +108,7 @@ def test_masks_of_the_lowest_value():
         x[0, :, 3:] = low                                            # fewer left than are asked for
         x[1, 0], x[1, 1, 0:4999], x[1, 2, 1:] = low, low, low        # every token of a row: all alike
         both(x, s, 6)
+        both(x, s, 4)
         both(x, s, 6, logit_scale=0.5)
 
 
@@ -162,6 +165,7 @@ def test_ended_rows_and_lengths(penalty):
     lens[3] = torch.tensor([0, -4, 1, 2 ** 31 - 2, 5], device="cuda", dtype=torch.int32)
     got = both(x, s, 7, finished=done, lengths=lens, length_penalty=penalty, end_token=700)
     assert got["finished"].dtype == torch.bool and bool(got["finished"][0, :5].all())
+    both(x[:, 1:], s[:, 1:].contiguous(), 4, finished=done[:, 1:].contiguous(), lengths=lens[:, 1:].contiguous(), length_penalty=penalty, end_token=700)
     both(x, s, 5, finished=done)                                     # no token of its own: -1 is reported
     both(x, s, 5, end_token=1233)
     both(x, s, 5, lengths=lens)
