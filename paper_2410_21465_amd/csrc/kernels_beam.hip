@@ -400,7 +400,7 @@ __device__ __forceinline__ RowSum row_sum(const BeamArgs& a, int row, int lane) 
   double sum = 0.0;
   for (int i = lane; i < a.n_parts; i += kWave) {
     const BeamPart q = parts[i];
-    sum += q.plain * exp2_f64(-(double)ref * c);
+    if (q.plain > 0.0) sum += q.plain * exp2_f64(-(double)ref * c);   // (then ref >= 0; otherwise the power may be anything)
     if (q.ref > -INFINITY) sum += q.sum * exp2_f64(((double)q.ref - (double)ref) * c);
   }
   return RowSum{log(wave_sum_f64_dpp(sum)), ref};

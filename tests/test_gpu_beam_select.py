@@ -101,6 +101,18 @@ def test_masks_that_leave_few_blocks(groups, beams, n):
     both(x, s, n)
 
 
+@pytest.mark.parametrize("n", [4, 6])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_of_very_low_logits(dtype, n):
+    """Nothing but logits far below zero: the row's sum is of what they are relative to the largest, whatever that is.  Thousands of rows, for
+    what depends on the lowest bits of a product."""
+    for seed, scale in enumerate((1.0, 0.7, 1.9)):
+        gen = torch.Generator(device="cuda").manual_seed(40 + seed)
+        x = (-10.0 ** (3.0 + 35.0 * torch.rand(3000, 4, 1, generator=gen, device="cuda"))).to(LOGIT_TYPES[dtype]).repeat(1, 1, 33)
+        x[1000:1500, :, 20:], x[1500:2000, :, 5:9] = -math.inf, torch.finfo(x.dtype).min
+        both(x, torch.zeros(3000, 4, device="cuda"), n, logit_scale=scale)
+
+
 def test_masks_of_the_lowest_value():
     for dtype in ("bf16", "fp16", "fp32"):
         x, s, _ = draw(2, 4, 5000, dtype, 12)
@@ -184,8 +196,12 @@ def test_outputs_in_place_of_inputs():
     for n in (65, -1, 2 ** 32 + 3):
         with pytest.raises(S.ShadowKVError):
             S.beam_select(x, s, n_out=n)
-    with pytest.raises(ValueError):
-        S.beam_select(x, s, end_token=2 ** 32)
+    for bad in (dict(end_token=2 ** 32), dict(lengths=lens[:, :5]), dict(lengths=lens.long()), dict(finished=done.int())):
+        with pytest.raises(ValueError):
+            S.beam_select(x, s, **bad)
+    for bad in (x.transpose(1, 2), x.double(), x[0], x[..., ::2]):
+        with pytest.raises(ValueError):
+            S.beam_select(bad, s)
     assert S.beam_select(x[:0], s[:0])["tokens"].shape == (0, 6)
 
 
