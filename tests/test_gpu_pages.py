@@ -197,6 +197,27 @@ def test_a_page_beyond_four_gib():
     assert bool((k[n - 1] == 1.5).all()) and bool((v[5] == 2.5).all()) and float(k[n - 2].abs().sum()) == 0.0
 
 
+@pytest.mark.parametrize("batch", [5, 1500])
+def test_tables_with_a_stride_and_counts_at_any_address(batch):
+    """The C interface's pool: rows of the table further apart than they are long, counts that are aligned to themselves only; what lies
+    between the rows is left alone."""
+    width, n_pages, ps = 6, 40 + 4 * batch, 4
+    pool, plain = S.PagePool(batch, width, n_pages, ps), PlainPool(batch, width, n_pages, ps)
+    wide = torch.full((batch, width + 3), 77, dtype=torch.int32, device="cuda")
+    pool.page_table = wide[:, :width].fill_(-1)
+    pool.page_refs = torch.full((n_pages + 2,), 0, dtype=torch.int32, device="cuda")[1:-1]
+    c = pool._c._obj
+    c.page_table, c.table_stride, c.page_refs = wide.data_ptr(), width + 3, pool.page_refs.data_ptr()
+    rng = random.Random(batch)
+    for turn in range(4):
+        step(pool, plain, [rng.randint(-1, batch - 1) for _ in range(batch)] if turn else None, None, [rng.randint(0, 9) for _ in range(batch)])
+        if turn % 2:
+            pool.compact()
+            plain.compact(1 << 30)
+            check_pool(pool, plain)
+    assert bool((wide[:, width:] == 77).all())
+
+
 def test_a_large_pool():
     n_pages, ps = 300001, 4
     pool, plain = S.PagePool(8, 60000, n_pages, ps), PlainPool(8, 60000, n_pages, ps)

@@ -91,6 +91,7 @@ def test_many_arrays_of_all_kinds():
         arrays.append(rand((12, *[(3,), (0,), (16, 8), (1 + 37 * i,)][i // 4 % 4]), dtype, i))
     check(arrays, parents)
     S.reorder_rows([], parents)
+    S.reorder_rows([torch.empty(0, 5, device="cuda")], ints([]))
 
 
 def test_a_row_beyond_four_gib():
