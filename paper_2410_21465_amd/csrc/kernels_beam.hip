@@ -683,7 +683,8 @@ BeamRange beam_range(double scale) {
   r.low = fits ? (float)(-800.0 / r.c) : INFINITY;
   r.high = fits ? (float)(900.0 / r.c) : -INFINITY;
   r.absent = fits ? (float)(-900.0 / r.c) : -INFINITY;
-  r.reach = (float)std::min(500.0 / r.c, 1e38);
+  // (rounding of fp32 can double a step that is not taken: 2^960 for each of 2^30 tokens stays in fp64's range)
+  r.reach = (float)std::min(480.0 / r.c, 1e38);
   return r;
 }
 int beam_blocks(int vocab) { return (int)(((int64_t)vocab + kBlock - 1) / kBlock); }

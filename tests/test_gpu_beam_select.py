@@ -113,6 +113,19 @@ def test_rows_of_very_low_logits(dtype, n):
         both(x, torch.zeros(3000, 4, device="cuda"), n, logit_scale=scale)
 
 
+@pytest.mark.parametrize("n", [4, 6])
+@pytest.mark.parametrize("scale", [1.0, 1.29, 1.31, 2.7])
+def test_large_logits_a_step_apart(n, scale):
+    """Around 2^32 fp32 has steps of 512: the next larger logit weighs up to 2^960 times as much, more than that moves the reference."""
+    x = torch.full((3, 4, 6000), 2.0 ** 32, device="cuda")
+    x[0, :, 1000:] += 512.0
+    x[1, 1:, ::7] += 512.0
+    x[1, 2:, 5000:5100] += 1024.0
+    x[2, :, 3000:] = -(2.0 ** 32)
+    x[2, 1:, 100:4000:3] = -math.inf
+    both(x, -torch.arange(12, device="cuda", dtype=torch.float32).view(3, 4), n, slack=2.0 ** -50 * 2.0 ** 33, logit_scale=scale)
+
+
 def test_masks_of_the_lowest_value():
     for dtype in ("bf16", "fp16", "fp32"):
         x, s, _ = draw(2, 4, 5000, dtype, 12)
