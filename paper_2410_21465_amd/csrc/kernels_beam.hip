@@ -186,7 +186,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(5, 5))) voi
       // the reference moves up only where 2^t might leave fp64's range
       if (__ballot(most > u.ref + sc.reach)) {
         const float to = wave_max_f32(most);
-        u.far *= exp2_f64(((double)u.ref - (double)to) * sc.c);
+        u.far *= exp2(((double)u.ref - (double)to) * sc.c);   // (not held to 2^-1000: the sum may be up to 2^990)
         u.ref = to;
       }
       if (u.ref > -INFINITY) {
@@ -382,7 +382,9 @@ __device__ __forceinline__ int top_items(Key key, int n_entries, int n, JoinRoom
   return sort_room<kTies>(room, n, tid);
 }
 
-// log of a row's sum of exponentials relative to `ref`, by a wave; ref = -inf: the row offers nothing
+// log of a row's sum of exponentials relative to `ref`, by a wave; ref = -inf: the row offers nothing.  Plain sums lie in 2^-800 .. 2^930, far ones
+// are 1 .. 2^990 of a reference that may be anywhere (a logit counts up to 2^960 before it moves its wave's).  So a power is taken in two halves
+// where it brings a far sum down by more than fp64's range, and vanishes only where what it stands for does: next to a plain sum of 2^-800 too.
 __device__ __forceinline__ RowSum row_sum(const BeamArgs& a, int row, int lane) {
   const BeamPart* parts = a.parts + (int64_t)row * a.n_parts;
   const double c = a.range.c;
@@ -400,8 +402,11 @@ __device__ __forceinline__ RowSum row_sum(const BeamArgs& a, int row, int lane) 
   double sum = 0.0;
   for (int i = lane; i < a.n_parts; i += kWave) {
     const BeamPart q = parts[i];
-    if (q.plain > 0.0) sum += q.plain * exp2_f64(-(double)ref * c);   // (then ref >= 0; otherwise the power may be anything)
-    if (q.ref > -INFINITY) sum += q.sum * exp2_f64(((double)q.ref - (double)ref) * c);
+    if (q.plain > 0.0) sum += q.plain * exp2(-(double)ref * c);   // (then ref >= 0; otherwise the power may be anything)
+    if (q.ref > -INFINITY) {
+      const double half = exp2(0.5 * ((double)q.ref - (double)ref) * c);
+      sum += q.sum * half * half;
+    }
   }
   return RowSum{log(wave_sum_f64_dpp(sum)), ref};
 }
