@@ -690,6 +690,13 @@ class PagedCache:
         self.c = CPagedCache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], page_table.data_ptr(),
                              page_table.stride(0), self.batch, page_table.shape[1], n, h, d, ps, _DTYPES[k.dtype], 0)
         self.address, self.n_pages, self.page_size = C.addressof(self.c), n, ps
+        self._copyable = False                            # whether ``_check_copyable`` has accepted it
+
+    def _check_copyable(self) -> None:
+        """Raises what ``pages_copy`` inside this cache would."""
+        one, none = (C.c_void_p * 1)(self.address), CPageMoves()
+        _check(lib().shadowkv_pages_copy(one, one, 1, C.byref(none), None))
+        self._copyable = True
 
 
 def dense_pages(k: torch.Tensor, v: torch.Tensor, page_size: int) -> PagedCache:
@@ -941,6 +948,10 @@ class PagePool:
         for c in caches:
             if c.page_size != self.page_size or c.n_pages < self.n_pages or c.device != self.device:
                 raise ValueError(f"a cache must have {self.n_pages} pages of {self.page_size} tokens on {self.device}")
+            if not c._copyable:                           # (before anything of the pool has changed)
+                c._check_copyable()
+        if len(caches) > 4096:
+            raise ValueError("more than 4096 caches")
         return caches
 
     def update(self, parents: Optional[torch.Tensor] = None, keep_lens: Optional[torch.Tensor] = None, n_new=0, caches=(), stream=None) -> None:
