@@ -960,8 +960,8 @@ class PagePool:
         ``paged_append`` wants it; a row that the pages do not suffice for gets none.  Copies, in every cache of ``caches``, the last pages that
         rows share and are about to write."""
         each = isinstance(n_new, torch.Tensor)
-        if not each and not 0 <= n_new <= _INT32:
-            raise ValueError(f"n_new must be in [0, 2^31), not {n_new}")
+        if not each and not (0 <= n_new <= _INT32 and n_new == int(n_new)):
+            raise ValueError(f"n_new must be a whole number in [0, 2^31), not {n_new}")
         for name, t in (("parents", parents), ("keep_lens", keep_lens), ("n_new", n_new if each else None)):
             if t is not None:
                 if t.numel() != self.batch:
@@ -979,8 +979,8 @@ class PagePool:
         """Moves the highest used pages into the lowest free ones (at most ``max_moves``), in every cache of ``caches``.  Returns ``n_used [1]``
         int32 on the device: all pages from there on are free."""
         room, caches = self.move_src.numel(), self._layers(caches)
-        if max_moves is not None and not 0 <= max_moves <= _INT32:
-            raise ValueError(f"max_moves must be in [0, 2^31), not {max_moves}")
+        if max_moves is not None and not (0 <= max_moves <= _INT32 and max_moves == int(max_moves)):
+            raise ValueError(f"max_moves must be a whole number in [0, 2^31), not {max_moves}")
         with _launch(self.device, stream) as st:
             _check(lib().shadowkv_pages_compact(self._c, room if max_moves is None else int(max_moves), self._compact_moves, self.n_used.data_ptr(),
                                                 self.workspace.data_ptr(), self.workspace.numel(), st))

@@ -26,3 +26,12 @@ def test_caches_that_cannot_be_copied_are_refused_first(bad):
             call(caches=[cache()])
         with pytest.raises(ValueError, match="4096"):
             call(caches=[cache()] * 4097)
+
+
+@pytest.mark.parametrize("bad", [0.5, 1.5, float("nan"), float("inf"), -1, 2 ** 31])
+def test_numbers_that_are_not_whole_are_refused(bad):
+    p = S.PagePool(2, 4, 16, 8, device="cpu")
+    with pytest.raises(ValueError, match="n_new"):
+        p.update(n_new=bad)
+    with pytest.raises(ValueError, match="max_moves"):
+        p.compact(max_moves=bad)
