@@ -224,19 +224,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(5, 5))) voi
 // What reaches a bound that n keys reach, and few others do, is put into LDS and sorted by counting, for each, what is larger.  Keys are 64 bits
 // wide, 0 is none; they come with a number, and of equal keys the lower number goes first (kTies; other keys are never equal).
 constexpr int kJoinThreads = 256;
-struct RowSum {
-  double log_sum;
-  float ref;
-};
 template <int T>
 struct __align__(16) JoinRoom {
   static constexpr int kRoom = T == kWave ? 128 : 256;
   uint64_t key[kRoom];
   uint32_t item[kRoom];
-  uint32_t upper[T];
+  uint32_t upper[T == kWave ? 4 : T];                     // (a wave reads its lanes)
   uint64_t best[64];                                      // what comes out, in order
   uint32_t best_item[64];
-  RowSum sum;
   uint32_t bound;
   int count, other;
 };
@@ -382,6 +377,10 @@ __device__ __forceinline__ int top_items(Key key, int n_entries, int n, JoinRoom
   return sort_room<kTies>(room, n, tid);
 }
 
+struct RowSum {
+  double log_sum;
+  float ref;
+};
 // log of a row's sum of exponentials relative to `ref`, by a wave; ref = -inf: the row offers nothing.  Plain sums lie in 2^-800 .. 2^930, far ones
 // are 1 .. 2^990 of a reference that may be anywhere (a logit counts up to 2^960 before it moves its wave's).  So a power is taken in two halves
 // where it brings a far sum down by more than fp64's range, and vanishes only where what it stands for does: next to a plain sum of 2^-800 too.
@@ -411,10 +410,10 @@ __device__ __forceinline__ RowSum row_sum(const BeamArgs& a, int row, int lane) 
   return RowSum{log(wave_sum_f64_dpp(sum)), ref};
 }
 
-// what a row offers, in order, n places, by a team
-template <int DT, int T>
-__device__ __forceinline__ void row_offers(const BeamArgs& a, int row, JoinRoom<T>& room, BeamOffer* offer, int tid) {
-  constexpr int EB = Logit<DT>::bytes, kEach = 8, kLanes = kBlock / kEach, kAtOnce = T / kLanes;
+// what a row offers, in order, n places, by a workgroup
+template <int DT>
+__device__ __forceinline__ void row_offers(const BeamArgs& a, int row, JoinRoom<kJoinThreads>& room, RowSum& shared_sum, BeamOffer* offer, int tid) {
+  constexpr int EB = Logit<DT>::bytes, kEach = 8, kLanes = kBlock / kEach, kAtOnce = kJoinThreads / kLanes;
   const int lane = tid & (kWave - 1), wave = tid >> 6, group = row / a.beams;
   const float s = a.scores[row];
   const bool lives = row_lives(s), done = a.finished && a.finished[row];
@@ -425,9 +424,9 @@ __device__ __forceinline__ void row_offers(const BeamArgs& a, int row, JoinRoom<
     count = 1;
     if (tid == 0) offer[0] = BeamOffer{f64_key((double)s / weight), s, a.end_token};
   } else if (lives) {
-    if (wave == T / kWave - 1) {                          // (the other waves of a workgroup go ahead)
+    if (wave == kJoinThreads / kWave - 1) {               // (the other waves go ahead)
       const RowSum sum = row_sum(a, row, lane);
-      if (lane == 0) room.sum = sum;
+      if (lane == 0) shared_sum = sum;
     }
     const uint8_t* p = a.logits + (int64_t)group * a.group_stride + (int64_t)(row % a.beams) * a.beam_stride;
     // (logit, ~number): among equal logits the lower token or block goes first
@@ -464,17 +463,17 @@ __device__ __forceinline__ void row_offers(const BeamArgs& a, int row, JoinRoom<
         bound = find_bound(mine, a.n, room, tid);
       }
       if (tid == 0) room.count = 0;
-      team_sync<T>();
+      __syncthreads();
       each_token([&](uint64_t k) { take(k, 0, k >= bound, room, lane); });
-      team_sync<T>();
-      if (__builtin_expect(room.count > JoinRoom<T>::kRoom, 0))
+      __syncthreads();
+      if (__builtin_expect(room.count > JoinRoom<kJoinThreads>::kRoom, 0))
         take_exactly<false>([&](int i, uint32_t& item) -> uint64_t {
           const int t = block(i / kBlock) * kBlock + i % kBlock;
           return t < a.vocab ? token_key(t, item) : 0;
         }, n_best * kBlock, a.n, bound, room, tid);
       count = sort_room<false>(room, a.n, tid);
     }
-    const RowSum sum = room.sum;
+    const RowSum sum = shared_sum;
     if (sum.ref == -INFINITY) count = 0;
     if (tid < count) {
       const double score = (double)s - sum.log_sum + a.scale * ((double)key_f32((uint32_t)(room.best[tid] >> 32)) - (double)sum.ref);
@@ -511,8 +510,7 @@ __device__ __forceinline__ void give_out(const BeamArgs& a, int group, const Bea
 }
 
 // of what the rows of a group offer, the best
-template <int T>
-__device__ __forceinline__ void choose(const BeamArgs& a, int group, const BeamOffer* all, JoinRoom<T>& room, int tid) {
+__device__ __forceinline__ void choose(const BeamArgs& a, int group, const BeamOffer* all, JoinRoom<kJoinThreads>& room, int tid) {
   const int found = top_items<true>([&](int i, uint32_t& item) -> uint64_t {
     item = (uint32_t)i;                                   // in order of rows, then of places
     return all[i].rank;
@@ -523,7 +521,8 @@ __device__ __forceinline__ void choose(const BeamArgs& a, int group, const BeamO
 template <int DT>
 __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
   __shared__ JoinRoom<kJoinThreads> room;
-  row_offers<DT>(a, blockIdx.x, room, a.offers + (int64_t)blockIdx.x * a.n, threadIdx.x);
+  __shared__ RowSum sum;
+  row_offers<DT>(a, blockIdx.x, room, sum, a.offers + (int64_t)blockIdx.x * a.n, threadIdx.x);
 }
 __global__ __launch_bounds__(kJoinThreads) void beam_choose_kernel(BeamArgs a) {
   __shared__ JoinRoom<kJoinThreads> room;
