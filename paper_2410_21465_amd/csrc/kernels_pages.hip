@@ -156,6 +156,10 @@ __device__ __forceinline__ uint32_t free_pages(const PoolArg& p, int p0) {
 constexpr int kListRoom = 2048;                           // free pages in LDS; more of them in the workspace
 constexpr int kForkInPlan = 1024;                         // rows that the plan forks by itself
 constexpr int kPlanHeld = 8;
+// Pages that a row which stays gives up one by one, by its thread; rows that give up more go with the forks, which costs a look at every column of theirs.
+// 256 rows of 252, captured, as events around a replay see it, 8 / 16 / 32 / 64 pages of each: 26.3 / 31.6 / 49.8 / 86.8 us one by one, 32.3 / 32.3 / 33.0 /
+// 33.8 with the forks.  All 65,536 pages of one row: 18.8 ms one by one, 33 us with the forks.
+constexpr int kFewCut = 16;
 // Entries of the page table that the plan's workgroup deals with by itself.  An update that forks half of its rows, captured: 64 rows of 70 entries 9.7 us,
 // and 13.9 with a launch for the forks; 256 of 252 13.0 and 15.1; 1000 of 64 14.5 and 22.1.  Compaction: 64 of 70 6.9 us, 8.0 with a launch that
 // rewrites the table; 256 of 64 13.7 and 9.9.
@@ -197,7 +201,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_grow_kernel(PoolArg p, con
     }
   }
   __syncthreads();
-  int cut_from = 0, cut_to = 0;                           // pages that a row which is its own parent gives up
+  int cut_from = 0, cut_to = 0;                           // the few pages that a row which is its own parent gives up
 #pragma unroll
   for (int k = 0; k < kRowsPerThread; ++k) {
     const int i = tid * rpt + k;
@@ -212,8 +216,8 @@ __global__ __launch_bounds__(kPlanThreads) void pages_grow_kernel(PoolArg p, con
         f.from = (uint16_t)from[k];
         f.had = held_pages(lens[i], p.shift);
         f.keeps = held_pages(kept[k], p.shift);
-        changes = from[k] != i && (f.had || f.keeps);
-        if (from[k] == i) { cut_from = f.keeps; cut_to = f.had; }
+        changes = from[k] == i ? f.had - f.keeps > kFewCut : (f.had || f.keeps);
+        if (from[k] == i && !changes) { cut_from = f.keeps; cut_to = f.had; }
       }
     }
     if constexpr (kFork) list_fork(f, changes, forks, &n_forks, &width);   // (a row a thread)
