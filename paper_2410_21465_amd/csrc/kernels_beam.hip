@@ -11,9 +11,9 @@
 // interpolation of degree 8 (off by 1.1e-12 at most), 2^round(t) added to the exponent's bits.  fp64 costs the vector pipes what fp32 costs.
 // Lanes take the same tokens in the same order in every row, whatever its address is, so rows of equal logits get equal sums.
 //
-// 32 x 16 rows of 256K bf16, 32 places: 86 + 15 + 7.5 us.  The first launch issues 19.5 vector instructions a logit, 14 of them the
-// exponential (without them it takes 61 us, reads at 4.4 TB/s; without its reads 86).  16 x 4 rows of 128K, 8 places: 9.4 + 8.2 + 4.0,
-// latencies for the most part.
+// 32 x 16 rows of 256K bf16, 32 places: 87 + 15 + 7.6 us.  The first launch issues 19.5 vector instructions a logit, 14 of them the
+// exponential, 12 of all in fp64: four cycles each, they fill 84 % of the cycles (at 2.19 GHz; what the others wait for is not known).  16 x 4 rows
+// of 128K, 8 places: 9.8 + 8.3 + 3.9, latencies for the most part.
 #include <algorithm>
 
 #include "../../include/shadowkv.h"
@@ -531,7 +531,8 @@ __global__ __launch_bounds__(kJoinThreads) void beam_choose_kernel(BeamArgs a) {
 // ---- small calls: both in one launch, two waves for each of a group's rows -----------------------------------------------------
 // One wave of a row finds its best tokens, the other its sum.  Few places out of few keys are taken one by one, without LDS: the largest of the
 // wave, n times, 0.6 us a place; a third launch costs 2.5 us on the host and 2 on the GPU.  Captured and replayed, rows of 32000: 10.8 us at 1 x 4 with 4
-// places and 13.2 in three launches, 11.6 and 15.5 at 64 x 2 with 2, but 14.7 and 13.1 at 1 x 4 with 8; a row at a time of 1000, 7.8 and 12.1.
+// places and 13.2 in three launches, 11.6 and 15.5 at 64 x 2 with 2, but 14.7 and 13.1 at 1 x 4 with 8; a row at a time of 1000, 7.8 and 12.1.  (Beams and
+// blocks end where a wave holds an offer a lane, and two keys a lane: nothing has been measured beyond.)
 constexpr int kFewBeams = 4, kFewInOne = 4, kFewBlocks = 128;
 struct Taken {
   uint64_t key;                                           // lane i: the i-th largest, 0 if there are fewer
@@ -674,8 +675,8 @@ hipError_t launch(const BeamArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Tokens of a part: as many chunks as leave 8192 waves, a third more than the chip holds.  (32 x 16 rows of 256K bf16, 8 / 16 / 32 chunks: 93.3 / 93.4 /
-// 99.8 us.)
+// Tokens of a part: as many chunks as leave 8192 waves, 60 % more than the 5120 that the chip holds of this kernel (5 a SIMD).  (32 x 16 rows of 256K
+// bf16, 8 / 16 / 32 chunks: 93.3 / 93.4 / 99.8 us; taken at this size alone, by an earlier form of the kernel.)
 int beam_part_len(int64_t rows, int vocab) {
   const int64_t per = (rows * (((int64_t)vocab + kChunk - 1) / kChunk) + 8191) / 8192;
   return (int)std::min<int64_t>(std::max<int64_t>(per, 1), 1024) * kChunk;

@@ -2,7 +2,7 @@
 // lengths and a count of holders per page; a page is free where its count is 0, and pages are given out lowest first, so what a call does
 // follows from its arguments alone.
 //
-// Planning is one workgroup's chain of dependent reads (lengths; table; counts) and prefix sums: 9.8 us for 16 x 4 beams over 1300 pages, 10.8
+// Planning is one workgroup's chain of dependent reads (lengths; table; counts) and prefix sums: 10.0 us for 16 x 4 beams over 1300 pages, 11.4
 // for 256 rows over 30000; more workgroups would need more launches, of 2 us each.  Copies are bound by memory: 1 GB of pages in 410 us (5.1
 // TB/s read and written).
 #include <algorithm>
@@ -161,8 +161,9 @@ constexpr int kPlanHeld = 8;
 // 33.8 with the forks.  All 65,536 pages of one row: 18.8 ms one by one, 33 us with the forks.
 constexpr int kFewCut = 16;
 // Entries of the page table that the plan's workgroup deals with by itself.  An update that forks half of its rows, captured: 64 rows of 70 entries 9.7 us,
-// and 13.9 with a launch for the forks; 256 of 252 13.0 and 15.1; 1000 of 64 14.5 and 22.1.  Compaction: 64 of 70 6.9 us, 8.0 with a launch that
-// rewrites the table; 256 of 64 13.7 and 9.9.
+// and 13.9 with a launch for the forks; 256 of 252 13.0 and 15.1; 1000 of 64 14.5 and 22.1 (one launch is the faster up to the border, and may be beyond
+// it; all entries of 8 x 8192 taken from their rows: 32 us, of 2 x 65,536 with the other launch 18).  Compaction: 64 of 70 6.9 us, 8.0 with a
+// launch that rewrites the table; 256 of 64 13.7 and 9.9.
 constexpr int64_t kForkEntries = 65536, kRenameEntries = 8192;
 
 // One workgroup.  A thread has rows tid * rpt ...: consecutive ones, so that prefix sums over threads are in order of rows.  kFork: the rows

@@ -870,7 +870,7 @@ def _rows(t: torch.Tensor, n: int, device) -> tuple:
 def reorder_rows(arrays, parents: torch.Tensor, stream=None) -> None:
     """Row i of every tensor of ``arrays`` (one tensor or several, ``[rows, ...]`` of any types; views such as ``A[:, prompt:]`` or
     ``k[:, :, -32:]`` too) becomes what row ``parents[i]`` was, in place.  ``parents`` int32, as many as rows (``[groups, beams]`` of
-    ``beam_select``, say); rows with a parent outside stay as they are."""
+    ``beam_select``, say); rows with a parent outside stay as they are.  The tensors are on the GPU: values in pinned memory cannot follow."""
     arrays = [arrays] if isinstance(arrays, torch.Tensor) else arrays
     n, dev = parents.numel(), parents.device
     _want(parents, "parents", torch.int32, parents.shape)
@@ -956,9 +956,9 @@ class PagePool:
 
     def update(self, parents: Optional[torch.Tensor] = None, keep_lens: Optional[torch.Tensor] = None, n_new=0, caches=(), stream=None) -> None:
         """Row i becomes the first ``min(kv_lens[parents[i]], keep_lens[i])`` tokens of what row ``parents[i]`` was (empty where that is
-        outside the batch), with room for ``n_new`` (a number, or int32 ``[batch]``) further ones, which ``kv_lens`` then counts, as
+        outside the batch), with room for ``n_new`` (a whole number, or int32 ``[batch]``) further ones, which ``kv_lens`` then counts, as
         ``paged_append`` wants it; a row that the pages do not suffice for gets none.  Copies, in every cache of ``caches``, the last pages that
-        rows share and are about to write."""
+        rows share and are about to write.  Nothing has changed where a call is refused."""
         each = isinstance(n_new, torch.Tensor)
         if not each and not (0 <= n_new <= _INT32 and n_new == int(n_new)):
             raise ValueError(f"n_new must be a whole number in [0, 2^31), not {n_new}")
